@@ -15,3 +15,6 @@ from .binding import (  # noqa: F401
     KNN_ERR_STATIC_SCRATCH_TOO_SMALL, KNN_STATIC_SCRATCH_BYTES, knn_search_static, knn_measure_mfma_peak,
     knn_search, knn_search_raw, knn_status_string, knn_workspace_bytes, library_path, load,
 )
+from .attn import (  # noqa: F401
+    ATTN_BF16, ATTN_F16, ATTN_MAX_D, ATTN_SYMBOLS, AttnPlan, attn_apply, attn_grad, attn_grad_plan, attn_plan,
+)

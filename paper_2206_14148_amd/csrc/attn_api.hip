@@ -1,0 +1,202 @@
+// C ABI of the attention product and its gradient (see include/attn.h for the contract).
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstring>
+
+#include "../../include/attn.h"
+#include "attn_kernels.h"
+#include "knn_config.h"
+
+namespace knn {  // api.hip
+void set_last_hip_error(hipError_t e, const char* what);
+hipEvent_t profile_mark(hipStream_t stream);
+void profile_close(hipEvent_t begin, hipStream_t stream, int kind);
+void profile_drop(hipEvent_t begin);
+}  // namespace knn
+
+namespace {
+
+constexpr int64_t kMostRows = (int64_t)1 << 30;
+
+// Workgroups that fill the GPU: two on a compute unit, and one of the kernel by keys, whose registers
+// are those of two.
+constexpr int64_t kWantRows = 2 * knn::kNumCU, kWantKeys = knn::kNumCU;
+// A range of keys is worth a workgroup of its own from this many on: its sums are written and read once more, 4 d bytes a
+// row each way, against 4 d bytes a key read.
+constexpr int64_t kLeastRange = 256;
+
+uint64_t part_bytes(int64_t n, int32_t hq, int32_t d, int64_t splits) {
+    return splits > 1 ? knn::align_up((uint64_t)splits * n * hq * (d + 2) * 4) : 0;
+}
+
+knn_status check_shape(int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t d, attn_plan_t* out) {
+    if (!out) return KNN_ERR_INVALID_ARG;
+    std::memset(out, 0, sizeof(*out));
+    if (n < 0 || m < 0 || hkv < 1 || hq < hkv || hq % hkv != 0 || d < 1) return KNN_ERR_INVALID_ARG;
+    if (d > ATTN_MAX_D || n > kMostRows || m > kMostRows || hq > 65535) return KNN_ERR_UNSUPPORTED;
+    // one workgroup for each tile and head, at most 64 ranges each
+    if ((n / attn::kTileRows + 1) * hq > (1 << 24) || (m / attn::kTileRows + 1) * hq > (1 << 24)) return KNN_ERR_UNSUPPORTED;
+    out->n = n;
+    out->m = m;
+    out->hq = hq;
+    out->hkv = hkv;
+    out->d = d;
+    out->tile_rows = attn::kTileRows;
+    out->n_splits = 1;
+    return KNN_OK;
+}
+
+knn_status hip_fail(hipError_t e, const char* what) {
+    knn::set_last_hip_error(e, what);
+    return KNN_ERR_HIP;
+}
+
+bool usable(const attn_rows_t* t, int64_t rows) {
+    if (!t || t->ld < 0 || t->hs < 0) return false;
+    return rows == 0 || t->data;
+}
+
+attn::Rows rows_of(const attn_rows_t* t, int32_t d) {
+    attn::Rows r;
+    r.data = static_cast<unsigned short*>(t->data);
+    r.ld = t->ld;
+    r.hs = t->hs;
+    r.wide = reinterpret_cast<uintptr_t>(t->data) % 16 == 0 && d % 8 == 0 && t->ld % 8 == 0 && t->hs % 8 == 0;
+    return r;
+}
+
+knn_status fill_problem(const attn_options_t* o, int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t d, attn::Problem* p) {
+    if (!o || (o->dtype != ATTN_BF16 && o->dtype != ATTN_F16) || (o->causal != 0 && o->causal != 1)) return KNN_ERR_INVALID_ARG;
+    if (!(o->scale > 0.0) || !std::isfinite(o->scale) || !(o->cap >= 0.0) || !std::isfinite(o->cap)) return KNN_ERR_INVALID_ARG;
+    if ((o->starts == nullptr) != (o->k_starts == nullptr)) return KNN_ERR_INVALID_ARG;
+    if (o->starts ? o->docs < 1 || o->docs >= ((int64_t)1 << 31) - 1 : o->docs != 0 && o->docs != 1) return KNN_ERR_INVALID_ARG;
+    std::memset(p, 0, sizeof(*p));
+    p->mask.starts = o->starts;
+    p->mask.k_starts = o->k_starts;
+    p->mask.prefix = o->causal ? o->prefix : nullptr;
+    p->mask.docs = o->starts ? (int)o->docs : 1;
+    p->mask.causal = o->causal;
+    p->mask.n = (int)n;
+    p->mask.m = (int)m;
+    p->hq = hq;
+    p->hkv = hkv;
+    p->d = d;
+    p->f16 = o->dtype == ATTN_F16;
+    p->scale = (float)o->scale;
+    p->cap = (float)o->cap;
+    p->slopes = o->slopes;
+    return KNN_OK;
+}
+
+knn_status check_workspace(const attn_plan_t& plan, const void* workspace, uint64_t workspace_bytes) {
+    if (plan.workspace_bytes == 0) return KNN_OK;
+    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % knn::kAlign != 0) return KNN_ERR_INVALID_ARG;
+    return workspace_bytes < plan.workspace_bytes ? KNN_ERR_WORKSPACE_TOO_SMALL : KNN_OK;
+}
+
+}  // namespace
+
+extern "C" knn_status attn_plan(int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t d, uint64_t mem_limit_bytes,
+                                attn_plan_t* out) {
+    const knn_status st = check_shape(n, m, hq, hkv, d, out);
+    if (st != KNN_OK) return st;
+    const int64_t tiles = (n + attn::kTileRows - 1) / attn::kTileRows * hq;
+    int64_t s = 1;
+    while (tiles > 0 && tiles * s < kWantRows && 2 * s <= attn::kMaxSplits && m / (2 * s) >= kLeastRange &&
+           part_bytes(n, hq, d, 2 * s) <= mem_limit_bytes)
+        s *= 2;
+    out->n_splits = (int32_t)s;
+    out->workspace_bytes = part_bytes(n, hq, d, s);
+    return KNN_OK;
+}
+
+extern "C" knn_status attn_grad_plan(int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t d, uint64_t mem_limit_bytes,
+                                     attn_plan_t* out) {
+    const knn_status st = check_shape(n, m, hq, hkv, d, out);
+    if (st != KNN_OK) return st;
+    const uint64_t sums = knn::align_up((uint64_t)n * hq * 4);
+    out->min_limit_bytes = sums;
+    if (mem_limit_bytes < sums) return KNN_ERR_MEM_LIMIT_TOO_SMALL;
+    const int64_t tiles = (m + attn::kTileRows - 1) / attn::kTileRows * hkv;
+    auto bytes = [&](int64_t s) { return s > 1 ? knn::align_up((uint64_t)s * 2 * m * hkv * d * 4) : 0; };
+    int64_t s = 1;
+    while (tiles > 0 && tiles * s < kWantKeys && 2 * s <= hq / hkv && 2 * s <= attn::kMaxSplits &&
+           sums + bytes(2 * s) <= mem_limit_bytes)
+        s *= 2;
+    out->n_splits = (int32_t)s;
+    out->workspace_bytes = sums + bytes(s);
+    return KNN_OK;
+}
+
+extern "C" knn_status attn_apply(const attn_rows_t* Q, const attn_rows_t* K, const attn_rows_t* V, int64_t n, int64_t m,
+                                 int32_t hq, int32_t hkv, int32_t d, const attn_options_t* options,
+                                 uint64_t mem_limit_bytes, void* workspace, uint64_t workspace_bytes,
+                                 const attn_rows_t* O, float* lse, void* hip_stream) {
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    attn_plan_t plan;
+    knn_status st = attn_plan(n, m, hq, hkv, d, mem_limit_bytes, &plan);
+    if (st != KNN_OK) return st;
+    attn::Problem p;
+    st = fill_problem(options, n, m, hq, hkv, d, &p);
+    if (st != KNN_OK) return st;
+    if (!usable(Q, n) || !usable(K, m) || !usable(V, m) || !usable(O, n)) return KNN_ERR_INVALID_ARG;
+    if (n == 0) return KNN_OK;
+    st = check_workspace(plan, workspace, workspace_bytes);
+    if (st != KNN_OK) return st;
+    p.q = rows_of(Q, d);
+    p.k = rows_of(K, d);
+    p.v = rows_of(V, d);
+    p.o = rows_of(O, d);
+    p.lse = lse;
+    p.splits = plan.n_splits;
+    p.partial = static_cast<float*>(workspace);
+    hipEvent_t t = knn::profile_mark(stream);
+    const hipError_t e = attn::launch_forward(p, stream);
+    if (e != hipSuccess) {
+        knn::profile_drop(t);
+        return hip_fail(e, "attention kernel");
+    }
+    knn::profile_close(t, stream, 1);
+    return KNN_OK;
+}
+
+extern "C" knn_status attn_grad(const attn_rows_t* Q, const attn_rows_t* K, const attn_rows_t* V, const attn_rows_t* O,
+                                const float* lse, const attn_rows_t* dO, int64_t n, int64_t m, int32_t hq,
+                                int32_t hkv, int32_t d, const attn_options_t* options, uint64_t mem_limit_bytes,
+                                void* workspace, uint64_t workspace_bytes, const attn_rows_t* dQ,
+                                const attn_rows_t* dK, const attn_rows_t* dV, void* hip_stream) {
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    attn_plan_t plan;
+    knn_status st = attn_grad_plan(n, m, hq, hkv, d, mem_limit_bytes, &plan);
+    if (st != KNN_OK) return st;
+    attn::Problem p;
+    st = fill_problem(options, n, m, hq, hkv, d, &p);
+    if (st != KNN_OK) return st;
+    if (!usable(Q, n) || !usable(K, m) || !usable(V, m) || !usable(O, n) || !usable(dO, n) || !usable(dQ, n) ||
+        !usable(dK, m) || !usable(dV, m) || (n > 0 && !lse))
+        return KNN_ERR_INVALID_ARG;
+    if (n == 0 && m == 0) return KNN_OK;
+    st = check_workspace(plan, workspace, workspace_bytes);
+    if (st != KNN_OK) return st;
+    p.q = rows_of(Q, d);
+    p.k = rows_of(K, d);
+    p.v = rows_of(V, d);
+    p.o = rows_of(O, d);
+    p.dO = rows_of(dO, d);
+    p.dq = rows_of(dQ, d);
+    p.dk = rows_of(dK, d);
+    p.dv = rows_of(dV, d);
+    p.lse = const_cast<float*>(lse);
+    p.splits = plan.n_splits;
+    p.rowsums = static_cast<float*>(workspace);
+    p.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + knn::align_up((uint64_t)n * hq * 4));
+    hipEvent_t t = knn::profile_mark(stream);
+    const hipError_t e = attn::launch_grad(p, stream);
+    if (e != hipSuccess) {
+        knn::profile_drop(t);
+        return hip_fail(e, "attention gradient kernels");
+    }
+    knn::profile_close(t, stream, 1);
+    return KNN_OK;
+}

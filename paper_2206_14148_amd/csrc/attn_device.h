@@ -1,0 +1,291 @@
+// Device-side helpers shared by the gfx950 attention kernels: matrix-core operands, tiles of 64 rows in
+// LDS, and the interval of keys (or rows) that a row (or key) sees.  Unnamed namespace: each translation
+// unit has its own copy.
+//
+// The layouts all follow from one choice.  v_mfma_f32_32x32x16 gives lane l of a 32 x 32 product the column
+// l % 32 and the rows 8 a + 4 (l / 32) + b (a, b = 0 .. 3, register 4 a + b), and takes from it, of its
+// second operand, column l % 32 and eight of sixteen values of k.  Which eight is free as long as both
+// operands agree.  So the transposed scores (keys x rows) are made, a lane holds sixteen scores of ONE row
+// (the softmax is within a lane, and one exchange with lane ^ 32), and its registers 8 s .. 8 s + 7 are,
+// rounded, the second operand of the next product over keys 16 s + 8 e + 4 (l / 32) + b, without any move.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "attn_kernels.h"
+
+namespace attn {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kInf = __builtin_huge_valf();
+
+struct Bf16 {
+    typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+    static constexpr unsigned kExponents = 0x7f807f80u, kOne = 0x3f80u;
+    static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ unsigned pack(float x, float y) {  // to nearest even
+        v2 r;
+        r[0] = (__bf16)x;
+        r[1] = (__bf16)y;
+        return __builtin_bit_cast(unsigned, r);
+    }
+    static __device__ __forceinline__ float low(unsigned w) { return __uint_as_float(w << 16); }
+    static __device__ __forceinline__ float high(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
+};
+
+struct F16 {
+    typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+    static constexpr unsigned kExponents = 0x7c007c00u, kOne = 0x3c00u;
+    static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ unsigned pack(float x, float y) {
+        v2 r;
+        r[0] = (_Float16)x;
+        r[1] = (_Float16)y;
+        return __builtin_bit_cast(unsigned, r);
+    }
+    static __device__ __forceinline__ float low(unsigned w) { return (float)__builtin_bit_cast(v2, w)[0]; }
+    static __device__ __forceinline__ float high(unsigned w) { return (float)__builtin_bit_cast(v2, w)[1]; }
+};
+
+// what lane ^ 32 holds, combined with one's own
+__device__ __forceinline__ u32x2 both_halves(float v) {
+    return __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+}
+__device__ __forceinline__ float max_of_halves(float v) {
+    const u32x2 r = both_halves(v);
+    return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float sum_of_halves(float v) {
+    const u32x2 r = both_halves(v);
+    return __uint_as_float(r.x) + __uint_as_float(r.y);
+}
+
+// smallest or largest over the wave of a value that is the same in lane l and lane l ^ 32
+__device__ __forceinline__ int wave_least(int v) {
+    for (int s = 16; s; s >>= 1) v = min(v, __shfl_xor(v, s));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_most(int v) {
+    for (int s = 16; s; s >>= 1) v = max(v, __shfl_xor(v, s));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+// ---- documents --------------------------------------------------------------------------------
+
+// The document that holds x, by its starts: the last one that begins at or before x; -1 if x lies outside all.
+__device__ __forceinline__ int document_of(const int* starts, int docs, int x) {
+    if (x < starts[0] || x >= starts[docs]) return -1;
+    int low = 0, high = docs;  // starts[low] <= x < starts[high]
+    while (high - low > 1) {
+        const int mid = (low + high) >> 1;
+        if (starts[mid] <= x)
+            low = mid;
+        else
+            high = mid;
+    }
+    return low;
+}
+
+__device__ __forceinline__ int clamp_to(int64_t x, int low, int high) {
+    return x < low ? low : x > high ? high : (int)x;
+}
+
+struct Document {
+    int qs, qe, ks, ke, prefix;
+    int64_t shift;  // row i stands at key i + shift
+};
+// (clamped: whatever the arrays hold, rows stay within 0 .. n and keys within 0 .. m)
+__device__ __forceinline__ Document document(const Mask& k, int c) {
+    Document e{0, k.n, 0, k.m, 0, 0};
+    int64_t last = k.n;
+    int64_t first = 0;
+    if (k.starts) {
+        first = k.starts[c];
+        last = k.starts[c + 1];
+        e.qs = clamp_to(first, 0, k.n);
+        e.qe = clamp_to(last, e.qs, k.n);
+        e.ks = clamp_to(k.k_starts[c], 0, k.m);
+        e.ke = clamp_to(k.k_starts[c + 1], e.ks, k.m);
+    }
+    if (k.prefix) e.prefix = max(k.prefix[c], 0);
+    e.shift = (int64_t)e.ke - last;
+    return e;
+}
+
+// What a row sees: keys lo .. hi - 1; it stands at key `at`.
+struct Span {
+    int lo, hi, at, inside;
+};
+__device__ __forceinline__ Span keys_of_row(const Mask& k, int i) {
+    Span s{0, 0, 0, 0};
+    if (i >= k.n) return s;
+    const int c = k.starts ? document_of(k.starts, k.docs, i) : 0;
+    if (c < 0) return s;
+    const Document e = document(k, c);
+    const int64_t at = i + e.shift;
+    s.inside = 1;
+    s.at = (int)at;
+    s.lo = e.ks;
+    s.hi = k.causal ? clamp_to(max(at + 1, (int64_t)e.ks + e.prefix), e.ks, e.ke) : e.ke;
+    return s;
+}
+// Which rows see a key: lo .. hi - 1; row i stands at key i + at.
+__device__ __forceinline__ Span rows_of_key(const Mask& k, int j) {
+    Span s{0, 0, 0, 0};
+    if (j >= k.m) return s;
+    const int c = k.starts ? document_of(k.k_starts, k.docs, j) : 0;
+    if (c < 0) return s;
+    const Document e = document(k, c);
+    s.inside = 1;
+    s.at = (int)e.shift;
+    s.hi = e.qe;
+    s.lo = k.causal && (int64_t)j >= (int64_t)e.ks + e.prefix ? clamp_to(j - e.shift, e.qs, e.qe) : e.qs;
+    return s;
+}
+
+// ---- tiles in LDS -----------------------------------------------------------------------------
+
+// 64 rows of DP entries (d rounded up; zeros behind d), row-major, a row 128 or 256 bytes.  Two readers: a
+// lane reads 16 bytes of row l % 32 (32 rows apart by whole rows: all in the same banks), and 16 lanes read
+// 32 bytes of each of 4 consecutive rows.  The 16-byte pieces of a row are therefore permuted by an exclusive-or
+// with bits of the row's number, (r1 r0 r2) below and r3 above: any eight rows in a run have different pieces, and
+// any four different pairs of pieces.
+template <int DP>
+struct Tile {
+    static constexpr int kPieces = DP <= 64 ? 8 : 16;  // of 16 bytes, in a row
+    static constexpr int kRowBytes = 16 * kPieces;
+    static constexpr int kBytes = kTileKeys * kRowBytes;
+    static __device__ __forceinline__ int turn(int row) {
+        const int t = ((row & 3) << 1) | ((row >> 2) & 1);
+        return kPieces == 16 ? t | (row & 8) : t;
+    }
+};
+
+// Eight entries from column c on, those at or behind d zero.
+__device__ __forceinline__ u32x4 entries8(const unsigned short* p, int c, int d, int wide) {
+    u32x4 r = {0, 0, 0, 0};
+    if (wide) {
+        if (c < d) r = *reinterpret_cast<const u32x4*>(p + c);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < d) r[e >> 1] |= (unsigned)p[c + e] << (16 * (e & 1));
+    }
+    return r;
+}
+
+// What a pass makes of entries that are not finite, before they meet weights that may be zero (see the kernels).
+enum Entries { kAsTheyAre = 0, kFinite = 1, kUp = 2, kDown = 3 };  // kUp, kDown: 1 for +infinity (-infinity) or NaN, else 0
+
+template <typename T>
+__device__ __forceinline__ unsigned chosen(unsigned w, int entries) {
+    constexpr unsigned kExp = T::kExponents & 0xffffu;
+    unsigned r = 0;
+#pragma unroll
+    for (int s = 0; s < 32; s += 16) {
+        const unsigned v = (w >> s) & 0xffffu;
+        const bool finite = (v & kExp) != kExp, none = !finite && (v & 0x7fffu) != kExp;
+        if (entries == kFinite)
+            r |= finite ? v << s : 0;
+        else if (!finite && (none || (v >> 15) == (entries == kDown)))
+            r |= T::kOne << s;
+    }
+    return r;
+}
+
+// Rows first .. first + 63 of one head into LDS; those outside lo .. hi - 1 become zeros.
+template <typename T, int DP, int THREADS>
+__device__ __forceinline__ void stage(unsigned char* lds, const Rows& t, int head, int first, int lo, int hi, int d, int tid,
+                                      int entries) {
+    typedef Tile<DP> L;
+    const unsigned short* base = t.data + head * t.hs;
+#pragma unroll
+    for (int it = 0; it < kTileKeys * L::kPieces / THREADS; ++it) {
+        const int at = it * THREADS + tid, r = at / L::kPieces, piece = (at % L::kPieces) ^ L::turn(r);
+        const int row = first + r;
+        u32x4 v = {0, 0, 0, 0};
+        if (row >= lo && row < hi) v = entries8(base + row * t.ld, 8 * piece, d, t.wide);
+        if (entries != kAsTheyAre)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = chosen<T>(v[e], entries);
+        *reinterpret_cast<u32x4*>(lds + at * 16) = v;
+    }
+}
+
+// First operand, rows as they are: row 32 part + l % 32 of the tile, entries 16 step + 8 (l / 32) ...
+template <int DP>
+__device__ __forceinline__ s16x8 rows_operand(const unsigned char* lds, int part, int step, int lane) {
+    typedef Tile<DP> L;
+    const int r = lane & 31;
+    const int piece = (2 * step + (lane >> 5)) ^ L::turn(r);
+    return *reinterpret_cast<const s16x8*>(lds + (32 * part + r) * L::kRowBytes + piece * 16);
+}
+
+// First operand, turned: column 32 block + l % 32 of the tile, rows 16 step + 8 e + 4 (l / 32) + b.  The
+// transposing read gives lane i of 16 the i-th of the 16 entries that lanes 4 b .. 4 b + 3 hold, b = 0 .. 3.
+template <int DP>
+__device__ __forceinline__ s16x8 columns_operand(const unsigned char* lds, int block, int step, int lane) {
+    typedef Tile<DP> L;
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const int b = (lane >> 2) & 3, half = lane >> 5;
+    const int piece = 4 * block + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+    s16x4 part[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int r = 8 * e + 4 * half + b;  // the row's last four bits
+        const unsigned char* p = lds + (16 * step + r) * L::kRowBytes + ((piece ^ L::turn(r)) * 16) + (lane & 1) * 8;
+        part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    }
+    return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Second operand from 16 numbers of a 32 x 32 product: registers 8 step .. 8 step + 7.
+template <typename T>
+__device__ __forceinline__ s16x8 rounded_operand(const f32x16& x, int step) {
+    u32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = T::pack(x[8 * step + 2 * e], x[8 * step + 2 * e + 1]);
+    return __builtin_bit_cast(s16x8, r);
+}
+
+// Workgroups go round the eight XCDs; runs of `total` / 8 consecutive pieces of work share one and its L2.
+__device__ __forceinline__ int work_of(int id, int total) {
+    const int q = total / 8, r = total % 8, x = id % 8, y = id / 8;
+    return x < r ? x * (q + 1) + y : r * (q + 1) + (x - r) * q + y;
+}
+
+// Four entries c .. c + 3 of a row to memory.
+template <typename T>
+__device__ __forceinline__ void put4(unsigned short* p, int c, int d, int wide, const float* x) {
+    const unsigned a = T::pack(x[0], x[1]), b = T::pack(x[2], x[3]);
+    if (wide) {
+        if (c < d) *reinterpret_cast<u32x2*>(p + c) = u32x2{a, b};
+    } else {
+        if (c < d) p[c] = (unsigned short)a;
+        if (c + 1 < d) p[c + 1] = (unsigned short)(a >> 16);
+        if (c + 2 < d) p[c + 2] = (unsigned short)b;
+        if (c + 3 < d) p[c + 3] = (unsigned short)(b >> 16);
+    }
+}
+
+}  // namespace
+
+}  // namespace attn

@@ -1,0 +1,252 @@
+// O = softmax(scores) V with a running maximum and sum: one pass over the keys, no n x m matrix.
+#include "attn_device.h"
+
+namespace attn {
+
+namespace {
+
+// The largest score of a row may grow by this many powers of two before its sums are scaled down to it.
+constexpr float kSlack = 8.f;
+
+// A lane's sums of its row to memory, or to the workspace as they are.  entries: see the walk below.
+template <typename T, int BLOCKS>
+__device__ __forceinline__ void write_rows(const Problem& p, const Span& see, int head, int row, int split, int half, int entries,
+                                           const f32x16* sum, float top, float total) {
+    const int64_t at = (int64_t)head * p.mask.n + row;
+    const float inverse = p.splits > 1 ? 1.f : total == 0.f ? 0.f : 1.f / total;
+    const int64_t rows = (int64_t)p.hq * p.mask.n;
+    float* const parts = p.partial + ((int64_t)split * rows + at) * p.d;
+    unsigned short* const o = p.o.data + row * p.o.ld + head * p.o.hs;
+    if (entries >= kUp) {
+        const float mark = entries == kUp ? kInf : -kInf;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int c = 32 * b + 8 * (e >> 2) + 4 * half + (e & 3);
+                if (c >= p.d || !(sum[b][e] > 0.f)) continue;
+                if (p.splits > 1)
+                    parts[c] += mark;
+                else
+                    o[c] = (unsigned short)T::pack(T::low(o[c]) + mark, 0.f);
+            }
+        return;
+    }
+    if (p.splits > 1) {
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int c = 32 * b + 8 * (e >> 2) + 4 * half + (e & 3);
+                if (c < p.d) parts[c] = sum[b][e];
+            }
+        if (half == 0) {
+            float* ends_of = p.partial + (int64_t)p.splits * rows * p.d + 2 * ((int64_t)split * rows + at);
+            ends_of[0] = top;
+            ends_of[1] = total;
+        }
+        return;
+    }
+    if (p.lse && half == 0) p.lse[at] = total == 0.f ? -kInf : (top + __builtin_amdgcn_logf(total)) * kLn2;
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = total == 0.f ? 0.f : sum[b][4 * a + e] * inverse;
+            put4<T>(o, 32 * b + 8 * a + 4 * half, p.d, p.o.wide, x);
+        }
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
+    typedef Tile<DP> L;
+    constexpr int kBlocks = DP / 32, kSteps = DP / 16;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[2 * L::kBytes];
+    __shared__ int ends[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int tiles = (p.mask.n + kTileRows - 1) / kTileRows;
+    const int w = work_of(blockIdx.x, gridDim.x);
+    // the last rows first: with a causal mask they see the most keys
+    const int split = w % p.splits, tile = tiles - 1 - w / p.splits % tiles, head = w / p.splits / tiles;
+    const int kv = head / (p.hq / p.hkv);
+    const int row = tile * kTileRows + wave * 32 + (lane & 31);
+    const Span see = keys_of_row(p.mask, row);
+    const bool some = see.lo < see.hi;
+    const int low = wave_least(some ? see.lo : INT_MAX), high = wave_most(some ? see.hi : INT_MIN);
+    // keys that all rows of the wave see (rows that are not written do not count)
+    const int all_low = wave_most(see.inside ? see.lo : INT_MIN), all_high = wave_least(see.inside ? see.hi : INT_MAX);
+    if (tid < 2) ends[tid] = tid ? INT_MIN : INT_MAX;
+    __syncthreads();
+    if (lane == 0) {
+        atomicMin(&ends[0], low);
+        atomicMax(&ends[1], high);
+    }
+    __syncthreads();
+    int first = ends[0], last = ends[1];
+    if (first >= last) first = last = 0;
+    const int steps = (last - first + kTileKeys - 1) / kTileKeys;
+    const int s0 = (int)((int64_t)steps * split / p.splits), s1 = (int)((int64_t)steps * (split + 1) / p.splits);
+
+    s16x8 q[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        u32x4 v = {0, 0, 0, 0};
+        if (see.inside) v = entries8(p.q.data + row * p.q.ld + head * p.q.hs, 16 * s + 8 * half, p.d, p.q.wide);
+        q[s] = __builtin_bit_cast(s16x8, v);
+    }
+    const bool general = p.cap > 0.f || p.slopes;
+    const float slope = p.slopes ? p.slopes[head] * kLog2e : 0.f;
+    const float factor = general ? 1.f : p.scale * kLog2e;  // of what the loop calls scores, to powers of two
+    const float slack = kSlack / factor;
+    const float to_cap = p.cap > 0.f ? 2.f * kLog2e * p.scale / p.cap : 0.f, from_cap = p.cap * kLog2e;
+
+    f32x16 sum[kBlocks];
+    float top, total;
+    // An infinity or a NaN in V meets the zero weights of rows that do not see it as well, and 0 * infinity is NaN.
+    // If any sum comes out not finite the workgroup walks three times more: with those entries as zeros, then with
+    // ones for what raises a sum to +infinity and to -infinity, whose sums are not zero for the rows that see one.
+    for (int entries = kAsTheyAre;; ++entries) {
+        for (int b = 0; b < kBlocks; ++b) sum[b] = f32x16{};
+        top = -kInf;
+        total = 0.f;
+        for (int s = s0; s < s1; ++s) {
+            const int j0 = first + s * kTileKeys;
+            __syncthreads();
+            stage<T, DP, 256>(lds, p.k, kv, j0, first, last, p.d, tid, kAsTheyAre);
+            stage<T, DP, 256>(lds + L::kBytes, p.v, kv, j0, first, last, p.d, tid, entries);
+            __syncthreads();
+            if (j0 >= high || j0 + kTileKeys <= low) continue;
+            f32x16 x[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                x[t] = f32x16{};
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k) x[t] = T::mfma(rows_operand<DP>(lds, t, k, lane), q[k], x[t]);
+            }
+            if (p.cap > 0.f) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        x[t][e] = from_cap * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * x[t][e])));
+            } else if (general) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[t][e] *= p.scale * kLog2e;
+            }
+            if (p.slopes) {
+                const float away = (float)(see.at - j0 - 4 * half);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        x[t][e] -= slope * fabsf(away - (float)(32 * t + 8 * (e >> 2) + (e & 3)));
+            }
+            if (j0 < all_low || j0 + kTileKeys > all_high) {
+                const unsigned width = (unsigned)(see.hi - see.lo);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if ((unsigned)(j0 + 4 * half + 32 * t + 8 * (e >> 2) + (e & 3) - see.lo) >= width) x[t][e] = -kInf;
+            }
+            float most = x[0][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) most = fmaxf(most, x[0][e]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) most = fmaxf(most, x[1][e]);
+            most = max_of_halves(most);
+            if (__any(most > top + slack)) {
+                const float now = fmaxf(top, most);
+                const float shrink = top == now ? 1.f : __builtin_amdgcn_exp2f((top - now) * factor);
+                top = now;
+                total *= shrink;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) sum[b] *= shrink;
+            }
+            const float base = top == -kInf ? 0.f : top;
+            s16x8 weights[4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    x[t][e] = __builtin_amdgcn_exp2f((x[t][e] - base) * factor);  // (the largest: 0, however large)
+                    total += x[t][e];
+                }
+                weights[2 * t] = rounded_operand<T>(x[t], 0);
+                weights[2 * t + 1] = rounded_operand<T>(x[t], 1);
+            }
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    sum[b] = T::mfma(columns_operand<DP>(lds + L::kBytes, b, k, lane), weights[k], sum[b]);
+        }
+        if (entries == kAsTheyAre) {
+            float zero = 0.f;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(sum[b][e], 0.f, zero);
+            if (__syncthreads_or(zero != 0.f)) continue;  // (NaN)
+        }
+        if (see.inside) write_rows<T, kBlocks>(p, see, head, row, split, half, entries, sum, top * factor, sum_of_halves(total));
+        if (entries == kAsTheyAre || entries == kDown) break;
+    }
+}
+
+// The ranges' sums of one row, in ascending order: a wave for each row and head.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_join_kernel(Problem p) {
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = (int64_t)p.hq * p.mask.n, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= rows) return;
+    const int head = (int)(at / p.mask.n), row = (int)(at % p.mask.n);
+    if (!keys_of_row(p.mask, row).inside) return;
+    const float* ends_of = p.partial + (int64_t)p.splits * rows * p.d;
+    float top = -kInf;
+    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, ends_of[2 * (s * rows + at)]);
+    const float base = top == -kInf ? 0.f : top;
+    float total = 0.f, x[2] = {0.f, 0.f};
+    for (int s = 0; s < p.splits; ++s) {
+        const float f = __builtin_amdgcn_exp2f(ends_of[2 * (s * rows + at)] - base);
+        total = __builtin_fmaf(ends_of[2 * (s * rows + at) + 1], f, total);
+        const float* o = p.partial + (s * rows + at) * p.d;
+        for (int e = 0; e < 2; ++e)
+            if (64 * e + lane < p.d && f != 0.f) x[e] = __builtin_fmaf(o[64 * e + lane], f, x[e]);
+    }
+    const float inverse = total == 0.f ? 0.f : 1.f / total;
+    for (int e = 0; e < 2; ++e)
+        if (64 * e + lane < p.d)
+            p.o.data[row * p.o.ld + head * p.o.hs + 64 * e + lane] =
+                (unsigned short)T::pack(total == 0.f ? 0.f : x[e] * inverse, 0.f);
+    if (p.lse && lane == 0) p.lse[at] = total == 0.f ? -kInf : (base + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
+template <typename T>
+hipError_t launch(const Problem& p, hipStream_t stream) {
+    const int64_t tiles = (p.mask.n + kTileRows - 1) / kTileRows;
+    const dim3 grid((unsigned)(tiles * p.hq * p.splits)), block(256);
+    if (p.d <= 64)
+        attn_forward_kernel<T, 64><<<grid, block, 0, stream>>>(p);
+    else if (p.d <= 96)
+        attn_forward_kernel<T, 96><<<grid, block, 0, stream>>>(p);
+    else
+        attn_forward_kernel<T, 128><<<grid, block, 0, stream>>>(p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    const int64_t rows = (int64_t)p.hq * p.mask.n;
+    attn_join_kernel<T><<<dim3((unsigned)((rows + 3) / 4)), block, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_forward(const Problem& p, hipStream_t stream) {
+    return p.f16 ? launch<F16>(p, stream) : launch<Bf16>(p, stream);
+}
+
+}  // namespace attn

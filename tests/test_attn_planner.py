@@ -1,0 +1,135 @@
+"""CPU-only: the attention library's symbols, plans and refusals (no GPU call is made)."""
+import ctypes
+import os
+import re
+
+import pytest
+
+import paper_2206_14148_amd as A
+from paper_2206_14148_amd import attn
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+GB = 10 ** 9
+
+
+def test_the_header_and_the_library_agree_on_the_symbols():
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "attn.h")).read(), flags=re.S)
+    names = set(re.findall(r"\b(attn_[a-z0-9_]+)\s*\(", text))
+    assert names == set(A.ATTN_SYMBOLS)
+    raw = ctypes.CDLL(A.library_path())
+    for name in names:
+        getattr(raw, name)
+
+
+def up(v):
+    return (v + 255) // 256 * 256
+
+
+@pytest.mark.parametrize("n,m,hq,hkv,d", [(1, 1, 1, 1, 1), (3, 50_021, 16, 2, 128), (8192, 8192, 32, 8, 128),
+                                         (100, 100_000, 4, 4, 64), (0, 5, 2, 1, 64), (5, 0, 2, 1, 64), (7, 1 << 30, 1, 1, 8)])
+def test_plans_stay_under_their_limit_and_count_what_they_keep(n, m, hq, hkv, d):
+    for limit in (0, 10 ** 4, 10 ** 6, GB, 1 << 40):
+        p = A.attn_plan(n, m, hq, hkv, d, limit)
+        assert p.workspace_bytes <= limit and p.min_limit_bytes == 0
+        assert p.workspace_bytes == (up(p.n_splits * n * hq * (d + 2) * 4) if p.n_splits > 1 else 0)
+        assert p.n_splits == 1 or m // p.n_splits >= 256
+        least = up(4 * n * hq)
+        if limit < least:
+            with pytest.raises(A.KnnError) as e:
+                A.attn_grad_plan(n, m, hq, hkv, d, limit)
+            assert e.value.status == A.KNN_ERR_MEM_LIMIT_TOO_SMALL and e.value.min_limit_bytes == least
+            continue
+        g = A.attn_grad_plan(n, m, hq, hkv, d, limit)
+        assert g.min_limit_bytes == least and 1 <= g.n_splits <= hq // hkv
+        assert g.workspace_bytes == least + (up(g.n_splits * 2 * m * hkv * d * 4) if g.n_splits > 1 else 0) <= limit
+
+
+def test_shapes_that_are_refused():
+    for plan in (A.attn_plan, A.attn_grad_plan):
+        for shape in [(-1, 5, 1, 1, 8), (5, -1, 1, 1, 8), (5, 5, 0, 1, 8), (5, 5, 1, 0, 8), (5, 5, 3, 2, 8), (5, 5, 1, 2, 8),
+                      (5, 5, 1, 1, 0)]:
+            with pytest.raises(A.KnnError) as e:
+                plan(*shape, GB)
+            assert e.value.status == A.KNN_ERR_INVALID_ARG
+        for shape in [(5, 5, 1, 1, 129), ((1 << 30) + 1, 5, 1, 1, 8), (5, (1 << 30) + 1, 1, 1, 8), (5, 5, 65536, 1, 8)]:
+            with pytest.raises(A.KnnError) as e:
+                plan(*shape, 1 << 60)
+            assert e.value.status == A.KNN_ERR_UNSUPPORTED
+
+
+def options(**other):
+    o = attn.OptionsStruct(dtype=0, causal=1, scale=0.1, cap=0.0, docs=1)
+    for k, v in other.items():
+        setattr(o, k, v)
+    return o
+
+
+def call(o=None, n=4, m=4, hq=2, hkv=1, d=64, ws=0x1000, ws_bytes=1 << 30, limit=GB, lse=0x1000, grad=False, **rows):
+    """Every call here is refused before anything is launched: the pointers are never followed."""
+    lib = attn._load()
+    t = {name: attn.RowsStruct(0x1000, 128, 64) for name in ("q", "k", "v", "out", "g", "dq", "dk", "dv")}
+    t.update(rows)
+    o = options() if o is None else o
+    if grad:
+        return lib.attn_grad(t["q"], t["k"], t["v"], t["out"], lse, t["g"], n, m, hq, hkv, d, o, limit, ws, ws_bytes,
+                             t["dq"], t["dk"], t["dv"], None)
+    return lib.attn_apply(t["q"], t["k"], t["v"], n, m, hq, hkv, d, o, limit, ws, ws_bytes, t["out"], lse, None)
+
+
+def test_calls_that_are_refused():
+    bad = [dict(dtype=2), dict(dtype=-1), dict(causal=2), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+           dict(scale=float("inf")), dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(starts=0x1000),
+           dict(k_starts=0x1000), dict(docs=2), dict(starts=0x1000, k_starts=0x1000, docs=0),
+           dict(starts=0x1000, k_starts=0x1000, docs=1 << 31)]
+    null, backward = attn.RowsStruct(None, 128, 64), attn.RowsStruct(0x1000, -1, 64)
+    for grad in (False, True):
+        for o in bad:
+            assert call(options(**o), grad=grad) == A.KNN_ERR_INVALID_ARG, o
+        for name in ("q", "k", "v", "out") + (("g", "dq", "dk", "dv") if grad else ()):
+            assert call(grad=grad, **{name: null}) == A.KNN_ERR_INVALID_ARG
+            assert call(grad=grad, **{name: backward}) == A.KNN_ERR_INVALID_ARG
+        assert call(d=129, grad=grad) == A.KNN_ERR_UNSUPPORTED
+    # few rows, many keys: parts in the workspace
+    assert call(m=100_000, ws=None) == A.KNN_ERR_INVALID_ARG
+    assert call(m=100_000, ws=0x1001) == A.KNN_ERR_INVALID_ARG
+    assert call(m=100_000, ws_bytes=10) == A.KNN_ERR_WORKSPACE_TOO_SMALL
+    assert call(grad=True, lse=None) == A.KNN_ERR_INVALID_ARG
+    assert call(grad=True, ws=None) == A.KNN_ERR_INVALID_ARG
+    assert call(grad=True, ws_bytes=0) == A.KNN_ERR_WORKSPACE_TOO_SMALL
+    assert call(grad=True, limit=0) == A.KNN_ERR_MEM_LIMIT_TOO_SMALL
+    lib = attn._load()
+    assert lib.attn_plan(4, 4, 2, 1, 64, GB, None) == A.KNN_ERR_INVALID_ARG
+    assert lib.attn_apply(None, None, None, 4, 4, 2, 1, 64, options(), GB, None, 0, None, None, None) == A.KNN_ERR_INVALID_ARG
+    assert lib.attn_apply(None, None, None, 4, 4, 2, 1, 64, None, GB, None, 0, None, None, None) == A.KNN_ERR_INVALID_ARG
+
+
+def test_the_binding_refuses_tensors_that_are_not_on_a_gpu():
+    torch = pytest.importorskip("torch")
+    q = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(A.KnnError) as e:
+        A.attn_apply(q, q, q, GB)
+    assert e.value.status == A.KNN_ERR_INVALID_ARG
+
+
+def test_the_formulas_gradients_against_differences():
+    """attn_formulas.py, which the kernels are held to: its gradients against central differences of its own O."""
+    torch = pytest.importorskip("torch")
+    from attn_formulas import attention
+
+    gen = torch.Generator().manual_seed(3)
+    n, m, hq, hkv, d = 11, 17, 2, 1, 5
+    Q, K, V, dO = (torch.randn(r, h, d, generator=gen, dtype=torch.float64) for r, h in
+                   ((n, hq), (m, hkv), (m, hkv), (n, hq)))
+    o = dict(causal=True, cap=2.0, slopes=[0.3, 0.1], starts=[0, 4, 11], k_starts=[0, 2, 17], prefix=[1, 5])
+    r = attention(Q, K, V, dO, **o)
+    for which, name in enumerate(("dQ", "dK", "dV")):
+        for _ in range(3):
+            way = torch.randn((Q, K, V)[which].shape, generator=gen, dtype=torch.float64)
+            step, value = 1e-5, []
+            for side in (step, -step):
+                data = [Q, K, V]
+                data[which] = data[which] + side * way
+                value.append(float((attention(*data, **o)["O"] * dO).sum()))
+            want = float((r[name] * way).sum())
+            # step^2 of a third derivative, and 2^-53 of sums of 110 terms over 2e-5
+            assert abs((value[0] - value[1]) / (2 * step) - want) < 1e-7 * (1 + abs(want))
