@@ -126,6 +126,99 @@ knn_status attn_grad(const attn_rows_t *Q, const attn_rows_t *K, const attn_rows
                      uint64_t workspace_bytes, const attn_rows_t *dQ, const attn_rows_t *dK, const attn_rows_t *dV,
                      void *hip_stream);
 
+/* ---- a cache of keys and values in 8 bits ------------------------------------------------------
+ *
+ * What answers one row at a time keeps the K and V of the rows before it.  Here they lie as 8-bit codes
+ * in blocks of `block` rows ("tokens"), in any order; a table gives each request its blocks, and every
+ * block has a scale for each head: a value is code * scale.  Half the bytes of 16-bit rows, and less
+ * than a hundredth on top for the scales: with a limit on device memory, twice the history.
+ *
+ *   k  [blocks][hkv][block][row]   codes, a token's entries together
+ *   v  [blocks][hkv][row][block]   codes, an entry's tokens together: the product with V sums over tokens
+ *   k_scale, v_scale  [blocks][hkv]  fp32, >= 0
+ * all DEVICE and contiguous, k and v 16-byte aligned.  row = attn_cache_row(d) entries, those behind d
+ * zero.  The slot of token t of block b is b * block + t.
+ */
+typedef enum { ATTN_INT8 = 0, ATTN_E4M3 = 1 } attn_code; /* -127 .. 127; OCP e4m3, up to 448 */
+
+typedef struct {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int64_t blocks;
+    int32_t hkv, d;
+    int32_t block; /* 16, 32, 64, 128 or 256 */
+    int32_t code;  /* attn_code */
+} attn_cache_t;
+
+/* HOST.  Entries of a row in the cache: 64 or 128; 0 where d < 1 or d > ATTN_MAX_D. */
+int32_t attn_cache_row(int32_t d);
+
+/*
+ * attn_cache_map - a step's block tables and slots, from the requests' lengths.
+ *   lengths [batch], news [batch]   DEVICE in, int32: tokens of each request after the step, and how many
+ *               of them are new (0 <= news <= lengths)
+ *   table [batch][width]   DEVICE in/out, int32: entries 0 .. ceil(before / block) - 1 of a request, before =
+ *               lengths - news, are its blocks already; those up to ceil(lengths / block) - 1 are written, with
+ *               the next entries of `free` for the requests in order.  The others are left as they were.
+ *   free [n_free]          DEVICE in, int32: blocks that no request has.  Where they run out -1 is written.
+ *   starts [batch + 1]     DEVICE out, int32: the new tokens of request i are rows starts[i] .. starts[i + 1] - 1
+ *   slots [n_slots]        DEVICE out, int64: where each goes; -1 where it has no block, and behind the last
+ *   used [1]               DEVICE out, int32: how many entries of `free` the step needs (more than n_free: too few)
+ * Lengths beyond width * block, and negative ones, are taken as the nearest that fits; news likewise.  Calling
+ * again with the same inputs writes the same.  batch <= 16384.  Errors: KNN_ERR_INVALID_ARG, KNN_ERR_UNSUPPORTED
+ * (batch, or width * block above 2^30), KNN_ERR_HIP.
+ */
+knn_status attn_cache_map(const int32_t *lengths, const int32_t *news, int64_t batch, int32_t *table, int64_t width,
+                          int32_t block, const int32_t *free, int64_t n_free, int32_t *starts, int64_t *slots,
+                          int64_t n_slots, int32_t *used, void *hip_stream);
+
+/*
+ * attn_cache_append - rows K [count][hkv][d], V [count][hkv][d] (DEVICE, of `dtype`) into the cache at
+ * slots [count] (DEVICE, int64).  Slots outside the cache (-1) are passed over.
+ * For each block and head with new tokens, K and V apart: a block that gets its token 0 is begun anew, all its
+ * codes zero and its scale 0.  scale' = max(scale, fl(a / most)), a the largest magnitude of the new rows,
+ * most = 127 or 448, fl to fp32.  If scale' > scale the codes there become the nearest to code * scale / scale'.
+ * A new code is the nearest to x / scale' (of two as near the even one; quotients of real numbers).
+ * NaN becomes 0 and an infinity the largest code; neither counts for a.
+ * The slots of one block must stand together in `slots`, in any order; of a slot given twice the last counts.
+ * Where one block's slots stand apart, what becomes of that block is not defined.
+ */
+knn_status attn_cache_append(const attn_cache_t *cache, int32_t dtype, const attn_rows_t *K, const attn_rows_t *V,
+                             int64_t count, const int64_t *slots, void *hip_stream);
+
+/*
+ * The plan of attn_cache_apply: the tokens of a request are cut into ranges of range_tokens that
+ * workgroups walk concurrently; with more than one range in width * block tokens their sums (fp32) lie
+ * in the workspace until a last kernel joins them in ascending order.
+ */
+typedef struct {
+    int64_t batch, longest; /* longest: width * block */
+    int32_t nq, hq, hkv, d;
+    int32_t range_tokens;
+    int32_t n_ranges;
+    uint64_t workspace_bytes; /* <= limit */
+    uint64_t min_limit_bytes; /* 0 */
+} attn_cache_plan_t;
+
+/* HOST.  batch, longest >= 0, nq >= 1, heads and d as attn_plan. */
+knn_status attn_cache_plan(int64_t batch, int32_t nq, int32_t hq, int32_t hkv, int32_t d, int64_t longest,
+                           uint64_t mem_limit_bytes, attn_cache_plan_t *out /* HOST */);
+
+/*
+ * attn_cache_apply - attention of the last nq rows of each request over the cache.
+ *   Q, O [batch * nq][hq][d]   DEVICE in / out, of `dtype`: row i * nq + t is the t-th of request i's last nq,
+ *                  at p = lengths[i] - nq + t; it sees the tokens j <= p (none where p < 0: O = 0)
+ *   table [batch][width], lengths [batch]   DEVICE in, int32.  Tokens whose table entry is no block of the cache
+ *                  are not seen; a length is at most width * block.
+ *   scale, cap, slopes   as in attn_options_t
+ * Scores, maxima, totals and sums are fp32.  A code is exact in 16 bits; probabilities are rounded to f16, times
+ * the ratio of their block's scale to the largest of 64 tokens' scales.
+ */
+knn_status attn_cache_apply(const attn_cache_t *cache, int32_t dtype, const attn_rows_t *Q, int64_t batch, int32_t nq,
+                            int32_t hq, const int32_t *table, int64_t width, const int32_t *lengths, double scale,
+                            double cap, const float *slopes, uint64_t mem_limit_bytes, void *workspace,
+                            uint64_t workspace_bytes, const attn_rows_t *O, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

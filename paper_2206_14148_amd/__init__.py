@@ -16,5 +16,7 @@ from .binding import (  # noqa: F401
     knn_search, knn_search_raw, knn_status_string, knn_workspace_bytes, library_path, load,
 )
 from .attn import (  # noqa: F401
-    ATTN_BF16, ATTN_F16, ATTN_MAX_D, ATTN_SYMBOLS, AttnPlan, attn_apply, attn_grad, attn_grad_plan, attn_plan,
+    ATTN_BF16, ATTN_E4M3, ATTN_F16, ATTN_INT8, ATTN_MAX_D, ATTN_SYMBOLS, AttnCache, AttnCachePlan, AttnPlan, attn_apply,
+    attn_cache_append, attn_cache_apply, attn_cache_map, attn_cache_plan, attn_cache_row, attn_grad, attn_grad_plan,
+    attn_plan,
 )

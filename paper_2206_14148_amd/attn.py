@@ -11,7 +11,10 @@ from .binding import KNN_ERR_HIP, KNN_ERR_INVALID_ARG, KNN_OK, KnnError, knn_sta
 ATTN_MAX_D = 128
 ATTN_BF16, ATTN_F16 = 0, 1
 
-ATTN_SYMBOLS = ("attn_plan", "attn_grad_plan", "attn_apply", "attn_grad")
+ATTN_INT8, ATTN_E4M3 = 0, 1
+
+ATTN_SYMBOLS = ("attn_plan", "attn_grad_plan", "attn_apply", "attn_grad", "attn_cache_row", "attn_cache_map",
+                "attn_cache_append", "attn_cache_plan", "attn_cache_apply")
 
 
 class RowsStruct(ctypes.Structure):
@@ -29,6 +32,33 @@ class AttnPlanStruct(ctypes.Structure):
                 ("d", ctypes.c_int32), ("tile_rows", ctypes.c_int32), ("n_splits", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64),
                 ("min_limit_bytes", ctypes.c_uint64)]
+
+
+class CacheStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("blocks", ctypes.c_int64), ("hkv", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("block", ctypes.c_int32), ("code", ctypes.c_int32)]
+
+
+class AttnCachePlanStruct(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("longest", ctypes.c_int64), ("nq", ctypes.c_int32), ("hq", ctypes.c_int32),
+                ("hkv", ctypes.c_int32), ("d", ctypes.c_int32), ("range_tokens", ctypes.c_int32),
+                ("n_ranges", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64),
+                ("min_limit_bytes", ctypes.c_uint64)]
+
+
+@dataclass(frozen=True)
+class AttnCachePlan:
+    batch: int
+    longest: int
+    nq: int
+    hq: int
+    hkv: int
+    d: int
+    range_tokens: int
+    n_ranges: int
+    workspace_bytes: int
+    min_limit_bytes: int
 
 
 @dataclass(frozen=True)
@@ -57,6 +87,13 @@ def _load():
         lib.attn_apply.argtypes = [rows, rows, rows] + shape + [ptr(OptionsStruct), u64, vp, u64, rows, vp, vp]
         lib.attn_grad.argtypes = [rows, rows, rows, rows, vp, rows] + shape + [ptr(OptionsStruct), u64, vp, u64, rows,
                                                                               rows, rows, vp]
+        cache = ptr(CacheStruct)
+        lib.attn_cache_row.argtypes = [i32]
+        lib.attn_cache_map.argtypes = [vp, vp, i64, vp, i64, i32, vp, i64, vp, vp, i64, vp, vp]
+        lib.attn_cache_append.argtypes = [cache, i32, rows, rows, i64, vp, vp]
+        lib.attn_cache_plan.argtypes = [i64, i32, i32, i32, i32, i64, u64, ptr(AttnCachePlanStruct)]
+        lib.attn_cache_apply.argtypes = [cache, i32, rows, i64, i32, i32, vp, i64, vp, ctypes.c_double, ctypes.c_double,
+                                         vp, u64, vp, u64, rows, vp]
         for name in ATTN_SYMBOLS:
             getattr(lib, name).restype = ctypes.c_int
         _ready = True
@@ -235,3 +272,173 @@ def attn_grad(Q, K, V, O, lse, dO, mem_limit_bytes: int, scale=None, causal: boo
     if st != KNN_OK:
         _raise(st)
     return dQ, dK, dV
+
+
+def attn_cache_row(d: int) -> int:
+    """Entries of a row in a cache of rows of d: 64 or 128."""
+    row = int(_load().attn_cache_row(d))
+    if row == 0:
+        _refuse(f"d must be in 1 .. {ATTN_MAX_D}")
+    return row
+
+
+@dataclass(frozen=True)
+class AttnCache:
+    """Keys and values of earlier rows as 8-bit codes in blocks: k [blocks, hkv, block, row], v [blocks, hkv, row,
+    block] (int8 or float8_e4m3fn, contiguous), k_scale, v_scale fp32 [blocks, hkv]; row = attn_cache_row(d)."""
+    k: "object"
+    v: "object"
+    k_scale: "object"
+    v_scale: "object"
+    d: int
+
+    @staticmethod
+    def empty(blocks: int, hkv: int, d: int, block: int, code: str = "int8", device="cuda") -> "AttnCache":
+        """A cache of nothing yet; code "int8" or "e4m3"."""
+        import torch
+
+        dtype = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[code]
+        row = attn_cache_row(d)
+        k = torch.zeros((blocks, hkv, block, row), dtype=torch.uint8, device=device).view(dtype)
+        v = torch.zeros((blocks, hkv, row, block), dtype=torch.uint8, device=device).view(dtype)
+        scales = [torch.zeros((blocks, hkv), dtype=torch.float32, device=device) for _ in range(2)]
+        return AttnCache(k, v, scales[0], scales[1], d)
+
+    @staticmethod
+    def blocks_within(limit_bytes: int, hkv: int, d: int, block: int) -> int:
+        """How many blocks limit_bytes hold, scales included."""
+        return _b.knn_chunk_rows(limit_bytes, hkv * (2 * block * attn_cache_row(d) + 8))
+
+    def _struct(self):
+        import torch
+
+        k, v = self.k, self.v
+        if k.dim() != 4 or v.dim() != 4 or not k.is_cuda:
+            _refuse("k and v must be 4-D device tensors")
+        blocks, hkv, block, row = k.shape
+        if row != attn_cache_row(self.d) or tuple(v.shape) != (blocks, hkv, row, block):
+            _refuse(f"k must be [blocks, hkv, block, {attn_cache_row(self.d)}] and v the same with the last two exchanged")
+        if k.dtype not in (torch.int8, torch.float8_e4m3fn) or v.dtype != k.dtype or v.device != k.device or \
+                not k.is_contiguous() or not v.is_contiguous():
+            _refuse("k and v must be contiguous, both int8 or both float8_e4m3fn, on one device")
+        for t in (self.k_scale, self.v_scale):
+            if t.dtype != torch.float32 or t.device != k.device or tuple(t.shape) != (blocks, hkv) or not t.is_contiguous():
+                _refuse("k_scale and v_scale must be contiguous float32 [blocks, hkv] on the device of k")
+        return CacheStruct(k.data_ptr(), v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), blocks, hkv,
+                           self.d, block, ATTN_INT8 if k.dtype == torch.int8 else ATTN_E4M3)
+
+
+def attn_cache_plan(batch: int, nq: int, hq: int, hkv: int, d: int, longest: int, mem_limit_bytes: int) -> AttnCachePlan:
+    ps = AttnCachePlanStruct()
+    st = int(_load().attn_cache_plan(batch, nq, hq, hkv, d, longest, mem_limit_bytes, ctypes.byref(ps)))
+    if st != KNN_OK:
+        _raise(st, ps)
+    return AttnCachePlan(*(getattr(ps, f[0]) for f in AttnCachePlanStruct._fields_))
+
+
+def _check_table(table, batch, device):
+    import torch
+
+    if not table.is_cuda or table.device != device or table.dtype != torch.int32 or table.dim() != 2 or \
+            table.shape[0] != batch or not table.is_contiguous():
+        _refuse(f"table must be contiguous int32 [{batch}, width] on {device}")
+
+
+def attn_cache_map(lengths, news, table, free, block: int, n_slots: int, out=None):
+    """attn_cache_map(lengths[batch], news[batch], table[batch,width], free[n], block, n_slots)
+    -> (table, starts int32 [batch+1], slots int64 [n_slots], used int32 [1]).
+
+    A step's block tables and slots from the requests' lengths after it and their numbers of new tokens (all int32):
+    `table` is completed in place with blocks from `free`, in order; the new tokens of request i are rows starts[i] ..
+    starts[i + 1] - 1 and go to slots; -1 behind the last and where there is no block.  `used` entries of `free` are
+    needed; more than it has: too few.  `out` takes (starts, slots, used).
+    """
+    import torch
+
+    if not lengths.is_cuda:
+        _refuse("lengths must be a device tensor (no CPU path exists)")
+    device, batch = lengths.device, lengths.numel()
+    _check_table(table, batch, device)
+    pointers = (_words("lengths", lengths, device, batch, torch.int32), _words("news", news, device, batch, torch.int32))
+    free_ptr = _words("free", free, device, None, torch.int32)
+    with torch.cuda.device(device):
+        if out is None:
+            starts = torch.empty((batch + 1,), dtype=torch.int32, device=device)
+            slots = torch.empty((n_slots,), dtype=torch.int64, device=device)
+            used = torch.empty((1,), dtype=torch.int32, device=device)
+        else:
+            starts, slots, used = out
+            _words("starts", starts, device, batch + 1, torch.int32)
+            _words("slots", slots, device, n_slots, torch.int64)
+            _words("used", used, device, 1, torch.int32)
+        st = int(_load().attn_cache_map(*pointers, batch, table.data_ptr(), table.shape[1], block, free_ptr, free.numel(),
+                                        starts.data_ptr(), slots.data_ptr(), n_slots, used.data_ptr(),
+                                        torch.cuda.current_stream(device).cuda_stream))
+    if st != KNN_OK:
+        _raise(st)
+    return table, starts, slots, used
+
+
+def attn_cache_append(cache: AttnCache, K, V, slots) -> None:
+    """attn_cache_append(cache, K[count,hkv,d], V[count,hkv,d], slots int64 [count]): new rows into the cache.
+
+    The slots of one block must stand together; -1 is passed over.  A block's scale grows with its largest magnitude,
+    codes that it holds already follow; a block that gets its token 0 is begun anew.
+    """
+    import torch
+
+    c = cache._struct()
+    if not K.is_cuda or K.device != cache.k.device:
+        _refuse("K and V must be on the cache's device")
+    dtype = _dtype(K)
+    if K.dim() != 3 or V.dim() != 3:
+        _refuse("K and V must be [rows, heads, d]")
+    count = K.shape[0]
+    _check_rows("K", K, K, (count, c.hkv, c.d))
+    _check_rows("V", V, K, (count, c.hkv, c.d))
+    at = _words("slots", slots, K.device, count, torch.int64)
+    with torch.cuda.device(K.device):
+        st = int(_load().attn_cache_append(c, dtype, _rows(K), _rows(V), count, at,
+                                           torch.cuda.current_stream(K.device).cuda_stream))
+    if st != KNN_OK:
+        _raise(st)
+
+
+def attn_cache_apply(Q, cache: AttnCache, table, lengths, mem_limit_bytes: int, scale=None, cap: float = 0.0, slopes=None,
+                     workspace=None, out=None):
+    """attn_cache_apply(Q[batch,nq,hq,d], cache, table int32 [batch,width], lengths int32 [batch], ...) -> O like Q.
+
+    Attention of the last nq rows of each request over the `lengths` tokens that the cache holds of it, the rows'
+    own among them: row t sees tokens up to lengths - nq + t.  scale, cap and slopes as in attn_apply.  The workspace
+    (uint8, attn_cache_plan's bytes for longest = width * block) is allocated here unless given.
+    """
+    import torch
+
+    c = cache._struct()
+    if not Q.is_cuda or Q.device != cache.k.device or Q.dim() != 4:
+        _refuse("Q must be [batch, nq, hq, d] on the cache's device")
+    dtype = _dtype(Q)
+    batch, nq, hq, d = Q.shape
+    if d != c.d or (d > 1 and Q.stride(3) != 1):
+        _refuse("Q must have the cache's d and unit stride along it")
+    _check_table(table, batch, Q.device)
+    at = _words("lengths", lengths, Q.device, batch, torch.int32)
+    tilt = _words("slopes", slopes, Q.device, hq, torch.float32)
+    plan = attn_cache_plan(batch, nq, hq, c.hkv, d, table.shape[1] * c.block, mem_limit_bytes)
+    with torch.cuda.device(Q.device):
+        workspace = _workspace(workspace, plan.workspace_bytes, Q.device)
+        O = torch.empty((batch, nq, hq, d), dtype=Q.dtype, device=Q.device) if out is None else out
+        if not O.is_cuda or O.device != Q.device or O.dtype != Q.dtype or O.shape != Q.shape or (d > 1 and O.stride(3) != 1):
+            _refuse(f"out must be {tuple(Q.shape)} in {Q.dtype} on {Q.device} with unit stride along its last dimension")
+        flat = []
+        for t in (Q, O):
+            if batch > 1 and nq > 1 and t.stride(0) != nq * t.stride(1):
+                _refuse("the rows of all requests must lie evenly apart (stride(0) == nq * stride(1))")
+            flat.append(RowsStruct(t.data_ptr() if t.numel() else None, t.stride(1) if nq > 1 else t.stride(0), t.stride(2)))
+        st = int(_load().attn_cache_apply(c, dtype, flat[0], batch, nq, hq, table.data_ptr(), table.shape[1], at,
+                                          1.0 / math.sqrt(d) if scale is None else float(scale), float(cap), tilt,
+                                          mem_limit_bytes, workspace.data_ptr(), workspace.numel(), flat[1],
+                                          torch.cuda.current_stream(Q.device).cuda_stream))
+    if st != KNN_OK:
+        _raise(st)
+    return O

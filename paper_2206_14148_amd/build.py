@@ -11,7 +11,7 @@ OBJ_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libknn_mi355x.so")
 SOURCES = ["planner.cpp", "api.hip", "knn_lowd.hip", "knn_grid.hip", "knn_few.hip", "knn_l1sad.hip", "knn_norms.hip", "knn_split.hip", "knn_packed.hip", "knn_wide.hip", "knn_refine.hip", "knn_peak.hip",
            "kmv_api.hip", "kmv_kernels.hip", "kmv_series.hip", "kmv_pieces.hip", "sgpr_api.hip", "sgpr_kernels.hip", "sgpr_pieces.hip",
-           "attn_api.hip", "attn_forward.hip", "attn_grad.hip"]
+           "attn_api.hip", "attn_forward.hip", "attn_grad.hip", "attn_cache.hip"]
 HEADERS = ["knn_config.h", "knn_device.h", "knn_cells.h", "knn_exact.h", "knn_kernels.h", "kmv_kernels.h", "sgpr_kernels.h", "attn_kernels.h", "attn_device.h",
            os.path.join("..", "..", "include", "attn.h"),
            os.path.join("..", "..", "include", "sgpr.h"),

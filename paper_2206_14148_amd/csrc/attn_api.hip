@@ -1,4 +1,4 @@
-// C ABI of the attention product and its gradient (see include/attn.h for the contract).
+// C ABI of the attention product, its gradient and its cache (see include/attn.h for the contract).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -196,6 +196,154 @@ extern "C" knn_status attn_grad(const attn_rows_t* Q, const attn_rows_t* K, cons
     if (e != hipSuccess) {
         knn::profile_drop(t);
         return hip_fail(e, "attention gradient kernels");
+    }
+    knn::profile_close(t, stream, 1);
+    return KNN_OK;
+}
+
+// ---- the cache --------------------------------------------------------------------------------
+
+namespace {
+
+bool cache_of(const attn_cache_t* c, attn::Cache* out) {
+    if (!c || c->hkv < 1 || c->blocks < 0 || c->blocks > kMostRows || attn_cache_row(c->d) == 0) return false;
+    if (c->block < 16 || c->block > 256 || (c->block & (c->block - 1)) != 0) return false;
+    if (c->code != ATTN_INT8 && c->code != ATTN_E4M3) return false;
+    if (c->blocks > 0 && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return false;
+    if (reinterpret_cast<uintptr_t>(c->k) % 16 != 0 || reinterpret_cast<uintptr_t>(c->v) % 16 != 0) return false;
+    out->k = static_cast<unsigned char*>(c->k);
+    out->v = static_cast<unsigned char*>(c->v);
+    out->k_scale = c->k_scale;
+    out->v_scale = c->v_scale;
+    out->blocks = c->blocks;
+    out->hkv = c->hkv;
+    out->d = c->d;
+    out->row = attn_cache_row(c->d);
+    out->block = c->block;
+    out->e4m3 = c->code == ATTN_E4M3;
+    return true;
+}
+
+// Tokens that one workgroup walks: so many ranges that the longest request alone, and the batch at about half
+// of its length, occupy the GPU, but no fewer tokens than its four waves take at once.
+constexpr int64_t kWantCache = 4 * knn::kNumCU;
+constexpr int64_t kLeastTokens = 256;
+
+}  // namespace
+
+extern "C" int32_t attn_cache_row(int32_t d) { return d < 1 || d > ATTN_MAX_D ? 0 : d <= 64 ? 64 : 128; }
+
+extern "C" knn_status attn_cache_map(const int32_t* lengths, const int32_t* news, int64_t batch, int32_t* table,
+                                     int64_t width, int32_t block, const int32_t* free, int64_t n_free,
+                                     int32_t* starts, int64_t* slots, int64_t n_slots, int32_t* used, void* hip_stream) {
+    if (batch < 0 || width < 0 || n_free < 0 || n_slots < 0 || block < 16 || block > 256 || (block & (block - 1)) != 0)
+        return KNN_ERR_INVALID_ARG;
+    if (batch > attn::kMostBatch || width > kMostRows / block) return KNN_ERR_UNSUPPORTED;
+    if (!starts || !used || (batch > 0 && (!lengths || !news)) || (batch > 0 && width > 0 && !table) ||
+        (n_free > 0 && !free) || (n_slots > 0 && !slots))
+        return KNN_ERR_INVALID_ARG;
+    attn::MapProblem p;
+    p.lengths = lengths;
+    p.news = news;
+    p.free = free;
+    p.table = table;
+    p.starts = starts;
+    p.used = used;
+    p.slots = slots;
+    p.n_slots = n_slots;
+    p.n_free = n_free;
+    p.batch = (int)batch;
+    p.width = (int)width;
+    p.block = block;
+    const hipError_t e = attn::launch_map(p, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? KNN_OK : hip_fail(e, "attention cache map kernel");
+}
+
+extern "C" knn_status attn_cache_append(const attn_cache_t* cache, int32_t dtype, const attn_rows_t* K, const attn_rows_t* V,
+                                        int64_t count, const int64_t* slots, void* hip_stream) {
+    attn::AppendProblem p;
+    if (!cache_of(cache, &p.cache) || (dtype != ATTN_BF16 && dtype != ATTN_F16) || count < 0) return KNN_ERR_INVALID_ARG;
+    if (!usable(K, count) || !usable(V, count) || (count > 0 && !slots)) return KNN_ERR_INVALID_ARG;
+    if (count > kMostRows || count * cache->hkv > ((int64_t)1 << 32)) return KNN_ERR_UNSUPPORTED;
+    if (count == 0 || cache->blocks == 0) return KNN_OK;
+    p.k = rows_of(K, cache->d);
+    p.v = rows_of(V, cache->d);
+    p.slots = slots;
+    p.count = count;
+    p.f16 = dtype == ATTN_F16;
+    const hipError_t e = attn::launch_append(p, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? KNN_OK : hip_fail(e, "attention cache append kernel");
+}
+
+extern "C" knn_status attn_cache_plan(int64_t batch, int32_t nq, int32_t hq, int32_t hkv, int32_t d, int64_t longest,
+                                      uint64_t mem_limit_bytes, attn_cache_plan_t* out) {
+    if (!out) return KNN_ERR_INVALID_ARG;
+    std::memset(out, 0, sizeof(*out));
+    if (batch < 0 || longest < 0 || nq < 1 || hkv < 1 || hq < hkv || hq % hkv != 0 || d < 1) return KNN_ERR_INVALID_ARG;
+    if (d > ATTN_MAX_D || longest > kMostRows || batch > kMostRows || hq > 65535 || nq > 65535) return KNN_ERR_UNSUPPORTED;
+    const int64_t rows = (int64_t)nq * (hq / hkv), per = rows > 16 ? 32 : 16;
+    if ((double)batch * hkv * ((rows + per - 1) / per) > (1 << 24)) return KNN_ERR_UNSUPPORTED;
+    const int64_t sets = batch * hkv * ((rows + per - 1) / per);
+    auto bytes = [&](int64_t ranges) {
+        return ranges > 1 ? knn::align_up((uint64_t)ranges * batch * nq * hq * (d + 2) * 4) : 0;
+    };
+    int64_t ranges = 1;
+    while (sets > 0 && sets * ranges < kWantCache && ranges < attn::kMaxSplits && longest / (2 * ranges) >= kLeastTokens &&
+           bytes(2 * ranges) <= mem_limit_bytes)
+        ranges *= 2;
+    const int64_t tokens = ((longest + ranges - 1) / ranges + kLeastTokens - 1) / kLeastTokens * kLeastTokens;
+    out->batch = batch;
+    out->longest = longest;
+    out->nq = nq;
+    out->hq = hq;
+    out->hkv = hkv;
+    out->d = d;
+    out->range_tokens = (int32_t)(tokens ? tokens : kLeastTokens);
+    out->n_ranges = tokens ? (int32_t)((longest + tokens - 1) / tokens) : 1;
+    out->workspace_bytes = bytes(out->n_ranges);
+    return KNN_OK;
+}
+
+extern "C" knn_status attn_cache_apply(const attn_cache_t* cache, int32_t dtype, const attn_rows_t* Q, int64_t batch,
+                                       int32_t nq, int32_t hq, const int32_t* table, int64_t width,
+                                       const int32_t* lengths, double scale, double cap, const float* slopes,
+                                       uint64_t mem_limit_bytes, void* workspace, uint64_t workspace_bytes,
+                                       const attn_rows_t* O, void* hip_stream) {
+    attn::CacheProblem p;
+    if (!cache_of(cache, &p.cache) || (dtype != ATTN_BF16 && dtype != ATTN_F16) || width < 0) return KNN_ERR_INVALID_ARG;
+    if (!(scale > 0.0) || !std::isfinite(scale) || !(cap >= 0.0) || !std::isfinite(cap)) return KNN_ERR_INVALID_ARG;
+    if (width > kMostRows / cache->block) return KNN_ERR_UNSUPPORTED;
+    attn_cache_plan_t plan;
+    const knn_status st = attn_cache_plan(batch, nq, hq, cache->hkv, cache->d, width * cache->block, mem_limit_bytes, &plan);
+    if (st != KNN_OK) return st;
+    if (!usable(Q, batch) || !usable(O, batch) || (batch > 0 && !lengths) || (batch > 0 && width > 0 && !table))
+        return KNN_ERR_INVALID_ARG;
+    if (batch == 0) return KNN_OK;
+    if (plan.workspace_bytes > 0) {
+        if (!workspace || reinterpret_cast<uintptr_t>(workspace) % knn::kAlign != 0) return KNN_ERR_INVALID_ARG;
+        if (workspace_bytes < plan.workspace_bytes) return KNN_ERR_WORKSPACE_TOO_SMALL;
+    }
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    p.q = rows_of(Q, cache->d);
+    p.o = rows_of(O, cache->d);
+    p.table = table;
+    p.lengths = lengths;
+    p.slopes = slopes;
+    p.partial = static_cast<float*>(workspace);
+    p.batch = (int)batch;
+    p.nq = nq;
+    p.hq = hq;
+    p.width = (int)width;
+    p.f16 = dtype == ATTN_F16;
+    p.ranges = plan.n_ranges;
+    p.range_tokens = plan.range_tokens;
+    p.scale = (float)scale;
+    p.cap = (float)cap;
+    hipEvent_t t = knn::profile_mark(stream);
+    const hipError_t e = attn::launch_cache(p, stream);
+    if (e != hipSuccess) {
+        knn::profile_drop(t);
+        return hip_fail(e, "attention cache kernel");
     }
     knn::profile_close(t, stream, 1);
     return KNN_OK;

@@ -1,0 +1,517 @@
+// Attention over a cache of 8-bit blocks, what writes the cache, and what finds its places.
+#include "attn_device.h"
+
+namespace attn {
+
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// ---- block tables and slots -------------------------------------------------------------------
+
+// Every workgroup sums up the whole batch by itself (a few words a request, from the L2) and then writes its own
+// part of the tables and slots: one launch, nothing to wait for.  New blocks are looked up in `free` and not in the
+// table, which another workgroup may be writing.
+constexpr int kMapThreads = 512;
+__global__ __launch_bounds__(kMapThreads) void attn_map_kernel(MapProblem p) {
+    extern __shared__ int sums[];  // [batch + 1] new tokens before a request, [batch + 1] new blocks
+    int* const tokens = sums;
+    int* const blocks = sums + p.batch + 1;
+    __shared__ int of_wave[2][kMapThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int most = p.width * p.block;
+    auto request = [&](int i, int& before, int& after) {
+        after = min(max(p.lengths[i], 0), most);
+        before = after - min(max(p.news[i], 0), after);
+    };
+    // sums of lengths are cut at 2^31 - 1: they only ever grow along the batch, and no place is past its request
+    auto plus = [](int a, int b) { return (int)min((unsigned)a + (unsigned)b, (unsigned)INT_MAX); };
+    int base_t = 0, base_b = 0;
+    for (int i0 = 0; i0 < p.batch; i0 += kMapThreads) {
+        const int i = i0 + tid;
+        int before = 0, after = 0;
+        if (i < p.batch) request(i, before, after);
+        int t = after - before, b = (after + p.block - 1) / p.block - (before + p.block - 1) / p.block;
+        for (int s = 1; s < 64; s <<= 1) {
+            const int x = __shfl_up(t, s), y = __shfl_up(b, s);
+            if (lane >= s) {
+                t = plus(t, x);
+                b = plus(b, y);
+            }
+        }
+        __syncthreads();
+        if (lane == 63) {
+            of_wave[0][wave] = t;
+            of_wave[1][wave] = b;
+        }
+        __syncthreads();
+        // those before this request: of the batch so far, of the waves before, of the lanes before
+        t = __shfl_up(t, 1);
+        b = __shfl_up(b, 1);
+        if (lane == 0) t = b = 0;
+        int all_t = base_t, all_b = base_b;
+        for (int w = 0; w < kMapThreads / 64; ++w) {
+            if (w == wave && i < p.batch) {
+                tokens[i] = plus(all_t, t);
+                blocks[i] = plus(all_b, b);
+            }
+            all_t = plus(all_t, of_wave[0][w]);
+            all_b = plus(all_b, of_wave[1][w]);
+        }
+        base_t = all_t;
+        base_b = all_b;
+    }
+    if (tid == 0) {
+        tokens[p.batch] = base_t;
+        blocks[p.batch] = base_b;
+    }
+    __syncthreads();
+    const int64_t at = (int64_t)blockIdx.x * kMapThreads + tid, step = (int64_t)gridDim.x * kMapThreads;
+    for (int64_t i = at; i <= p.batch; i += step) p.starts[i] = tokens[i];
+    if (at == 0) *p.used = base_b;
+    auto free_block = [&](int64_t i) { return i < p.n_free ? p.free[i] : -1; };
+    // new blocks, each by the request whose sum it falls into
+    auto owner = [&](const int* of, int64_t x) {  // the last request with of[i] <= x
+        int low = 0, high = p.batch;
+        while (high - low > 1) {
+            const int mid = (low + high) >> 1;
+            if (of[mid] <= x)
+                low = mid;
+            else
+                high = mid;
+        }
+        return low;
+    };
+    for (int64_t x = at; x < base_b; x += step) {
+        const int i = owner(blocks, x);
+        int before, after;
+        request(i, before, after);
+        p.table[(int64_t)i * p.width + (before + p.block - 1) / p.block + (x - blocks[i])] = free_block(x);
+    }
+    for (int64_t x = at; x < p.n_slots; x += step) {
+        int64_t slot = -1;
+        if (x < base_t) {
+            const int i = owner(tokens, x);
+            int before, after;
+            request(i, before, after);
+            const int j = before + (int)(x - tokens[i]), held = (before + p.block - 1) / p.block, b = j / p.block;
+            const int block = b < held ? p.table[(int64_t)i * p.width + b] : free_block(blocks[i] + (int64_t)(b - held));
+            if (block >= 0) slot = (int64_t)block * p.block + j % p.block;
+        }
+        p.slots[x] = slot;
+    }
+}
+
+// ---- new rows ---------------------------------------------------------------------------------
+
+__device__ __forceinline__ float value_of(unsigned code, int e4m3) {
+    return e4m3 ? __builtin_amdgcn_cvt_f32_fp8(code, 0) : (float)(signed char)code;
+}
+
+// The code nearest to y; y is exact or rounded to odd (its last bit says that something was cut off), so that the
+// one rounding here is that of the real number.
+__device__ __forceinline__ unsigned code_of(float y, int e4m3) {
+    if (!(fabsf(y) >= 0.f)) return 0;  // NaN
+    if (e4m3) return __builtin_amdgcn_cvt_pk_fp8_f32(fminf(fmaxf(y, -448.f), 448.f), 0.f, 0, false) & 0xffu;
+    return (unsigned)(int)__builtin_rintf(fminf(fmaxf(y, -127.f), 127.f)) & 0xffu;
+}
+
+__device__ __forceinline__ float quotient(float x, float s) {
+    if (s == 0.f) return 0.f;
+    const float y = x / s;
+    const unsigned bits = __float_as_uint(y);
+    if ((bits & 1) || !(fabsf(y) < kInf)) return y;
+    const float rest = __builtin_fmaf(-y, s, x);  // exact: its sign says on which side of y the quotient lies
+    if (rest == 0.f) return y;
+    return __uint_as_float((rest < 0.f) == (y < 0.f) ? bits | 1 : bits - 1);
+}
+
+__device__ __forceinline__ float quotient_of(float code, float from, float to) {
+    const double y = (double)code * from / to;
+    float f = (float)y;
+    if (fabs((double)f) > fabs(y)) f = __uint_as_float(__float_as_uint(f) - 1);
+    if ((double)f != y) f = __uint_as_float(__float_as_uint(f) | 1);
+    return f;
+}
+
+template <typename T>
+__device__ __forceinline__ float entry(const unsigned short* p) {
+    return T::low(*p);
+}
+
+// A wave for each new row and head; that of the first row of a run of rows that go to one block does the run.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_append_kernel(AppendProblem p) {
+    const Cache& c = p.cache;
+    const int lane = threadIdx.x & 63;
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), first = w / c.hkv;
+    const int head = (int)(w % c.hkv);
+    if (first >= p.count) return;
+    const int64_t slots = c.blocks * c.block;
+    auto block_of = [&](int64_t t) {
+        const int64_t s = p.slots[t];
+        return s >= 0 && s < slots ? s / c.block : -1;
+    };
+    const int64_t block = block_of(first);
+    if (block < 0 || (first > 0 && block_of(first - 1) == block)) return;
+    int64_t last = first + 1;
+    while (last < p.count && block_of(last) == block) ++last;
+
+    bool fresh = false;
+    float a[2] = {0.f, 0.f};
+    for (int64_t t = first; t < last; ++t) {
+        fresh |= p.slots[t] % c.block == 0;
+        for (int col = lane; col < c.d; col += 64)
+            for (int x = 0; x < 2; ++x) {
+                const Rows& r = x ? p.v : p.k;
+                const float v = fabsf(entry<T>(r.data + t * r.ld + head * r.hs + col));
+                if (v < kInf) a[x] = fmaxf(a[x], v);
+            }
+    }
+    for (int x = 0; x < 2; ++x) {
+        for (int s = 32; s; s >>= 1) a[x] = fmaxf(a[x], __shfl_xor(a[x], s));
+        float* const scale = (x ? c.v_scale : c.k_scale) + block * c.hkv + head;
+        unsigned char* const codes = (x ? c.v : c.k) + (block * c.hkv + head) * (int64_t)c.block * c.row;
+        const float before = fresh ? 0.f : *scale, after = fmaxf(before, a[x] / (c.e4m3 ? 448.f : 127.f));
+        if (fresh || after > before) {
+            for (int i = 4 * lane; i < c.block * c.row; i += 256) {
+                unsigned word = 0;
+                if (before > 0.f) {
+                    word = *reinterpret_cast<const unsigned*>(codes + i);
+                    unsigned moved = 0;
+                    for (int b = 0; b < 32; b += 8)
+                        moved |= code_of(quotient_of(value_of(word >> b & 0xffu, c.e4m3), before, after), c.e4m3) << b;
+                    word = moved;
+                }
+                *reinterpret_cast<unsigned*>(codes + i) = word;
+            }
+            if (lane == 0) *scale = after;
+            // other lanes write the new codes into those words
+            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "agent");
+        }
+        for (int64_t t = first; t < last; ++t) {
+            const Rows& r = x ? p.v : p.k;
+            const int token = (int)(p.slots[t] % c.block);
+            for (int col = lane; col < c.d; col += 64) {
+                const unsigned code = code_of(quotient(entry<T>(r.data + t * r.ld + head * r.hs + col), after), c.e4m3);
+                codes[x ? col * c.block + token : token * c.row + col] = (unsigned char)code;
+            }
+        }
+    }
+}
+
+// ---- attention over the cache -----------------------------------------------------------------
+
+// Eight codes to an operand of 16-bit numbers; every code is exact in either type.
+template <bool E4M3>
+__device__ __forceinline__ f16x8 halves_of(u32x2 w) {
+    f16x8 r;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        if constexpr (E4M3) {
+            const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], 1.f, false);
+            const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], 1.f, true);
+            r[4 * e] = a[0], r[4 * e + 1] = a[1], r[4 * e + 2] = b[0], r[4 * e + 3] = b[1];
+        } else {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) r[4 * e + b] = (_Float16)(short)(signed char)(w[e] >> (8 * b));
+        }
+    }
+    return r;
+}
+template <typename T, bool E4M3>
+__device__ __forceinline__ f32x4 codes_mfma(u32x2 w, s16x8 q, f32x4 c) {
+    if constexpr (T::kOne == F16::kOne) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<E4M3>(w), __builtin_bit_cast(f16x8, q), c, 0, 0, 0);
+    } else {
+        bf16x8 r;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if constexpr (E4M3) {
+                const Bf16::v2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], 1.f, false);
+                const Bf16::v2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], 1.f, true);
+                r[4 * e] = a[0], r[4 * e + 1] = a[1], r[4 * e + 2] = b[0], r[4 * e + 3] = b[1];
+            } else {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) r[4 * e + b] = (__bf16)(float)(signed char)(w[e] >> (8 * b));
+            }
+        }
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(r, __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
+    }
+}
+
+// A wave takes 64 tokens at a time, and 16 SETS rows: those of the heads that share a K and V, and of the nq rows.
+// Codes go from memory to registers in the order in which v_mfma_f32_16x16x32 takes them: lane l of a product has
+// column l % 16 (a row) and rows 4 (l / 16) + r.  K: operand row i of product t is token 16 (i / 4) + 4 t + i % 4, so
+// that the lanes of group g = l / 16 get the scores of tokens 16 g .. 16 g + 15, which lie in one block; a lane reads
+// its quarter of a token's row.  V: a lane reads one entry's tokens 16 g .. 16 g + 15, 16 bytes, and its scores,
+// rounded, are the other operand as they are.  Nothing goes through LDS until the four waves' sums meet.
+template <typename T, bool E4M3, int ROW, int SETS>
+__global__ __launch_bounds__(256) void attn_cache_kernel(CacheProblem p) {
+    constexpr int kSteps = ROW / 32, kTiles = ROW / 16;
+    __shared__ float of_waves[4][16 * SETS][ROW + 4];
+    __shared__ float ends[4][16 * SETS][2];
+    const Cache& c = p.cache;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
+    const int group = p.hq / c.hkv, rows = p.nq * group, row_sets = (rows + 16 * SETS - 1) / (16 * SETS);
+    const int w = work_of(blockIdx.x, gridDim.x);
+    const int range = w % p.ranges, set = w / p.ranges % row_sets, head = w / p.ranges / row_sets % c.hkv;
+    const int b = w / p.ranges / row_sets / c.hkv;
+    const int length = min(max(p.lengths[b], 0), p.width * c.block);
+    const int begin = range * p.range_tokens, end = min(length, begin + p.range_tokens);
+    // (of an empty request the first range writes the rows)
+    if (begin >= length && range > 0) return;
+    const int* const table = p.table + (int64_t)b * p.width;
+
+    s16x8 q[SETS][kSteps];
+    int hi[SETS];       // a row sees tokens below this
+    float slope[SETS];
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+        const int r = (set * SETS + s) * 16 + col, t = r / group, h = head * group + r % group;
+        hi[s] = r < rows ? length - p.nq + t + 1 : 0;
+        slope[s] = p.slopes && r < rows ? p.slopes[h] * kLog2e : 0.f;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            u32x4 v = {0, 0, 0, 0};
+            if (r < rows)
+                v = entries8(p.q.data + ((int64_t)b * p.nq + t) * p.q.ld + h * p.q.hs, g * (ROW / 4) + 8 * k, c.d, p.q.wide);
+            q[s][k] = __builtin_bit_cast(s16x8, v);
+        }
+    }
+    const float to_cap = p.cap > 0.f ? 2.f * kLog2e * p.scale / p.cap : 0.f, from_cap = p.cap * kLog2e;
+    const int seen_by_all = length - p.nq + 1;  // tokens below this are seen by every row
+
+    f32x4 sum[SETS][kTiles];
+    float top[SETS], total[SETS];
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+        top[s] = -kInf;
+        total[s] = 0.f;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) sum[s][t] = f32x4{};
+    }
+    const int64_t block_bytes = (int64_t)c.block * ROW;
+    auto block_at = [&](int j) {  // the block that holds token j, or -1
+        const int x = j < end ? table[j / c.block] : -1;
+        return x >= 0 && x < c.blocks ? x : -1;
+    };
+    for (int j0 = begin + 64 * wave; j0 < end; j0 += 256) {
+        // this lane's token of K: 16 (col / 4) + 4 t + col % 4; of V and of the scores: 16 g + ...
+        const int jk = j0 + 16 * (col >> 2), jv = j0 + 16 * g;
+        const int bk = block_at(jk), bv = block_at(jv);
+        const bool whole = j0 + 64 <= seen_by_all && j0 + 64 <= end && !__any(bv < 0);
+        u32x4 kc[4][ROW / 64], vc[kTiles];
+        const unsigned char* kp = c.k + (bk * (int64_t)c.hkv + head) * block_bytes + ((jk + (col & 3)) % c.block) * ROW + g * (ROW / 4);
+        const unsigned char* vp = c.v + (bv * (int64_t)c.hkv + head) * block_bytes + col * c.block + jv % c.block;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < ROW / 64; ++e)
+                kc[t][e] = bk >= 0 ? *reinterpret_cast<const u32x4*>(kp + 4 * t * ROW + 16 * e) : u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+            vc[t] = bv >= 0 ? *reinterpret_cast<const u32x4*>(vp + 16 * t * c.block) : u32x4{0, 0, 0, 0};
+        const float ks = bv >= 0 ? c.k_scale[bv * (int64_t)c.hkv + head] : 0.f;
+        const float vs = bv >= 0 ? c.v_scale[bv * (int64_t)c.hkv + head] : 0.f;
+        if (!whole && jv + 16 > end) {
+            // codes behind the last token may be anything, NaN among it
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int left = end - jv - 4 * e;  // tokens of this word
+                    vc[t][e] &= left >= 4 ? ~0u : left <= 0 ? 0u : ~0u >> (8 * (4 - left));
+                }
+        }
+        float vmost = fmaxf(vs, __shfl_xor(vs, 16));
+        vmost = fmaxf(vmost, __shfl_xor(vmost, 32));
+        const float share = vmost > 0.f ? vs / vmost : 0.f;
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) {
+            f32x4 x[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                x[t] = f32x4{};
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k)
+                    x[t] = codes_mfma<T, E4M3>(u32x2{kc[t][k / 2][2 * (k % 2)], kc[t][k / 2][2 * (k % 2) + 1]}, q[s][k], x[t]);
+            }
+            const float factor = p.scale * kLog2e * ks;
+            if (p.cap > 0.f) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[t][e] = from_cap * __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * ks * x[t][e])), 1.f);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) x[t] *= factor;
+            }
+            if (p.slopes) {
+                const float away = (float)(hi[s] - 1 - jv);
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[t][e] = __builtin_fmaf(-slope[s], away - (float)(4 * t + e), x[t][e]);
+            }
+            if (!whole) {
+                const int left = bv >= 0 ? min(hi[s], end) - jv : 0;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (4 * t + e >= left) x[t][e] = -kInf;
+            }
+            float most = x[0][0];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = fmaxf(most, x[t][e]);
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const float now = fmaxf(top[s], most), base = now == -kInf ? 0.f : now;
+            const float shrink = __builtin_amdgcn_exp2f(top[s] - base);
+            top[s] = now;
+            total[s] *= shrink;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[t][e] = __builtin_amdgcn_exp2f(x[t][e] - base);
+                    total[s] += x[t][e];
+                }
+            f16x8 weights[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) weights[u][e] = (_Float16)(x[2 * u + e / 4][e % 4] * share);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                f32x4 y{};
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<E4M3>(u32x2{vc[t][0], vc[t][1]}), weights[0], y, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<E4M3>(u32x2{vc[t][2], vc[t][3]}), weights[1], y, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[s][t][e] = __builtin_fmaf(y[e], vmost, sum[s][t][e] * shrink);
+            }
+        }
+    }
+    // the four waves' sums, in their order
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+        total[s] += __shfl_xor(total[s], 16);
+        total[s] += __shfl_xor(total[s], 32);
+        if (g == 0) {
+            ends[wave][16 * s + col][0] = top[s];
+            ends[wave][16 * s + col][1] = total[s];
+        }
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) *reinterpret_cast<f32x4*>(&of_waves[wave][16 * s + col][16 * t + 4 * g]) = sum[s][t];
+    }
+    __syncthreads();
+    const int64_t all = (int64_t)p.batch * c.hkv * rows;
+    for (int i = tid; i < 16 * SETS * ROW; i += 256) {
+        const int r = i / ROW, d = i % ROW, row = set * 16 * SETS + r;
+        if (row >= rows || d >= c.d) continue;
+        float most = -kInf, whole = 0.f, y = 0.f;
+        for (int x = 0; x < 4; ++x) most = fmaxf(most, ends[x][r][0]);
+        const float base = most == -kInf ? 0.f : most;
+        for (int x = 0; x < 4; ++x) {
+            const float f = __builtin_amdgcn_exp2f(ends[x][r][0] - base);
+            whole = __builtin_fmaf(ends[x][r][1], f, whole);
+            y = __builtin_fmaf(of_waves[x][r][d], f, y);
+        }
+        if (p.ranges > 1) {
+            const int64_t at = ((int64_t)b * c.hkv + head) * rows + row;
+            p.partial[(range * all + at) * c.d + d] = y;
+            if (d == 0) {
+                float* const e = p.partial + p.ranges * all * c.d + 2 * (range * all + at);
+                e[0] = most;
+                e[1] = whole;
+            }
+        } else {
+            unsigned short* const o = p.o.data + ((int64_t)b * p.nq + row / group) * p.o.ld + (head * group + row % group) * p.o.hs;
+            o[d] = (unsigned short)T::pack(whole == 0.f ? 0.f : y / whole, 0.f);
+        }
+    }
+}
+
+// The ranges' sums of one row in ascending order: a wave for each.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_cache_join_kernel(CacheProblem p) {
+    const Cache& c = p.cache;
+    const int lane = threadIdx.x & 63, group = p.hq / c.hkv, rows = p.nq * group;
+    const int64_t all = (int64_t)p.batch * c.hkv * rows, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= all) return;
+    const int row = (int)(at % rows), head = (int)(at / rows % c.hkv), b = (int)(at / rows / c.hkv);
+    const int length = min(max(p.lengths[b], 0), p.width * c.block);
+    const int ranges = max(1, (length + p.range_tokens - 1) / p.range_tokens);
+    const float* const ends_of = p.partial + p.ranges * all * c.d;
+    float top = -kInf;
+    for (int s = 0; s < ranges; ++s) top = fmaxf(top, ends_of[2 * (s * all + at)]);
+    const float base = top == -kInf ? 0.f : top;
+    float total = 0.f, x[2] = {0.f, 0.f};
+    for (int s = 0; s < ranges; ++s) {
+        const float f = __builtin_amdgcn_exp2f(ends_of[2 * (s * all + at)] - base);
+        total = __builtin_fmaf(ends_of[2 * (s * all + at) + 1], f, total);
+        for (int e = 0; e < 2; ++e)
+            if (64 * e + lane < c.d) x[e] = __builtin_fmaf(p.partial[(s * all + at) * c.d + 64 * e + lane], f, x[e]);
+    }
+    unsigned short* const o = p.o.data + ((int64_t)b * p.nq + row / group) * p.o.ld + (head * group + row % group) * p.o.hs;
+    for (int e = 0; e < 2; ++e)
+        if (64 * e + lane < c.d) o[64 * e + lane] = (unsigned short)T::pack(total == 0.f ? 0.f : x[e] / total, 0.f);
+}
+
+template <typename T, bool E4M3, int ROW>
+hipError_t launch(const CacheProblem& p, hipStream_t stream) {
+    const int group = p.hq / p.cache.hkv, rows = p.nq * group;
+    const int sets = rows > 16 ? 2 : 1;
+    const int64_t workgroups = (int64_t)p.batch * p.cache.hkv * ((rows + 16 * sets - 1) / (16 * sets)) * p.ranges;
+    if (sets == 1)
+        attn_cache_kernel<T, E4M3, ROW, 1><<<dim3((unsigned)workgroups), dim3(256), 0, stream>>>(p);
+    else
+        attn_cache_kernel<T, E4M3, ROW, 2><<<dim3((unsigned)workgroups), dim3(256), 0, stream>>>(p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.ranges == 1) return e;
+    const int64_t all = (int64_t)p.batch * p.cache.hkv * rows;
+    attn_cache_join_kernel<T><<<dim3((unsigned)((all + 3) / 4)), dim3(256), 0, stream>>>(p);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch(const CacheProblem& p, hipStream_t stream) {
+    if (p.cache.row == 64) return p.cache.e4m3 ? launch<T, true, 64>(p, stream) : launch<T, false, 64>(p, stream);
+    return p.cache.e4m3 ? launch<T, true, 128>(p, stream) : launch<T, false, 128>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_map(const MapProblem& p, hipStream_t stream) {
+    const size_t lds = 2 * ((size_t)p.batch + 1) * 4;
+    if (lds > 48 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_map_kernel),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    const int64_t work = p.n_slots > p.batch + 1 ? p.n_slots : p.batch + 1;
+    int64_t grid = (work + kMapThreads - 1) / kMapThreads;
+    if (grid > 256) grid = 256;
+    attn_map_kernel<<<dim3((unsigned)grid), dim3(kMapThreads), lds, stream>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t launch_append(const AppendProblem& p, hipStream_t stream) {
+    const dim3 grid((unsigned)((p.count * p.cache.hkv + 3) / 4));
+    if (p.f16)
+        attn_append_kernel<F16><<<grid, dim3(256), 0, stream>>>(p);
+    else
+        attn_append_kernel<Bf16><<<grid, dim3(256), 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache(const CacheProblem& p, hipStream_t stream) {
+    return p.f16 ? launch<F16>(p, stream) : launch<Bf16>(p, stream);
+}
+
+}  // namespace attn

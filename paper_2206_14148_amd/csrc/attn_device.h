@@ -15,6 +15,10 @@
 
 #include "attn_kernels.h"
 
+// Products and sums are fused only where it is written: a score that is rounded once for the maximum and left
+// unrounded for the exponential is off by 2^-24 of itself there, however large it is.
+#pragma clang fp contract(off)
+
 namespace attn {
 
 namespace {

@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        x[t][e] = from_cap * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * x[t][e])));
+                        x[t][e] = from_cap * __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * x[t][e])), 1.f);
             } else if (general) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        x[t][e] -= slope * fabsf(away - (float)(32 * t + 8 * (e >> 2) + (e & 3)));
+                        x[t][e] = __builtin_fmaf(-slope, fabsf(away - (float)(32 * t + 8 * (e >> 2) + (e & 3))), x[t][e]);
             }
             if (j0 < all_low || j0 + kTileKeys > all_high) {
                 const unsigned width = (unsigned)(see.hi - see.lo);

@@ -25,11 +25,11 @@ struct Scores {
     __device__ __forceinline__ float score(float u, float away, float& steep) const {
         float s = u * factor;
         if (capped) {
-            const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * u));
+            const float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * u)), 1.f);
             s = from_cap * t;
-            steep = 1.f - t * t;
+            steep = __builtin_fmaf(-t, t, 1.f);
         }
-        return s - slope * fabsf(away);
+        return __builtin_fmaf(-slope, fabsf(away), s);
     }
 };
 

@@ -36,4 +36,44 @@ struct Problem {
 hipError_t launch_forward(const Problem& p, hipStream_t stream);
 hipError_t launch_grad(const Problem& p, hipStream_t stream);
 
+// ---- the cache (attn_cache.hip) ---------------------------------------------------------------
+
+struct Cache {
+    unsigned char *k, *v;
+    float *k_scale, *v_scale;
+    int64_t blocks;
+    int hkv, d, row, block, e4m3;
+};
+
+constexpr int kMostBatch = 16384;  // of a map: their new blocks and tokens are summed up in LDS
+
+struct MapProblem {
+    const int *lengths, *news, *free;
+    int *table, *starts, *used;
+    int64_t* slots;
+    int64_t n_slots, n_free;
+    int batch, width, block;
+};
+hipError_t launch_map(const MapProblem& p, hipStream_t stream);
+
+struct AppendProblem {
+    Cache cache;
+    Rows k, v;
+    const int64_t* slots;
+    int64_t count;
+    int f16;
+};
+hipError_t launch_append(const AppendProblem& p, hipStream_t stream);
+
+struct CacheProblem {
+    Cache cache;
+    Rows q, o;
+    const int *table, *lengths;
+    const float* slopes;
+    float* partial;
+    int batch, nq, hq, width, f16, ranges, range_tokens;
+    float scale, cap;
+};
+hipError_t launch_cache(const CacheProblem& p, hipStream_t stream);
+
 }  // namespace attn

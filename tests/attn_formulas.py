@@ -114,3 +114,117 @@ def compare(name, got, r):
                              f"want {float(want[tuple(at)])} within {float(most[tuple(at)])}")
     fine = look & torch.isfinite(want)
     return float(((got - want).abs()[fine] / most[fine].clamp(min=1e-300)).max()) if fine.any() else 0.0
+
+
+# ---- the cache ------------------------------------------------------------------------------
+
+def positive_codes(code):
+    """The values of the codes without a sign, ascending."""
+    if code == "int8":
+        return torch.arange(128, dtype=torch.float64)
+    return torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
+
+
+MOST = {"int8": 127.0, "e4m3": 448.0}
+
+
+def nearest(y, code):
+    """The codes' values nearest to 64-bit numbers, of two as near the one of even number; NaN to 0."""
+    whole = positive_codes(code)
+    a = torch.nan_to_num(y.abs(), nan=0.0).clamp(max=float(whole[-1]))
+    above = torch.searchsorted(whole, a.contiguous()).clamp(max=len(whole) - 1)
+    below = (above - 1).clamp(min=0)
+    up, down = whole[above] - a, a - whole[below]
+    take = (up < down) | ((up == down) & (above % 2 == 0))
+    return torch.copysign(torch.where(take, whole[above], whole[below]), torch.nan_to_num(y, nan=0.0)) + 0.0
+
+
+def append(k, v, k_scale, v_scale, K, V, slots, d, block, code):
+    """The cache's code values (float64, k [N][h][block][row], v [N][h][row][block]) and scales (fp32) after an append."""
+    out = []
+    runs = {}
+    for t, s in enumerate(slots):
+        if 0 <= s < k.shape[0] * block:
+            runs.setdefault(s // block, []).append((s % block, t))
+    for codes, scale, x in ((k.clone(), k_scale.clone(), K), (v.transpose(2, 3).clone(), v_scale.clone(), V)):
+        x = x.detach().cpu().double()
+        for b, rows in runs.items():
+            for h in range(x.shape[1]):
+                new = x[[t for _, t in rows], h]
+                size = torch.where(torch.isfinite(new), new.abs(), torch.zeros_like(new))
+                s0 = torch.zeros(()) if any(o == 0 for o, _ in rows) else scale[b, h].clone()
+                s1 = torch.maximum(s0, (size.max().float() / torch.tensor(MOST[code])))
+                if float(s0) == 0.0 and any(o == 0 for o, _ in rows):
+                    codes[b, h] = 0.0
+                elif s1 > s0:
+                    codes[b, h] = nearest(codes[b, h] * s0.double() / s1.double(), code)
+                for o, t in rows:
+                    y = x[t, h] / s1.double() if float(s1) > 0 else torch.zeros_like(x[t, h])
+                    codes[b, h, o, :d] = nearest(y, code)
+                scale[b, h] = s1
+        out += [codes, scale]
+    return out[0], out[2].transpose(2, 3), out[1], out[3]
+
+
+def cache_map(lengths, news, table, free, block, n_slots):
+    table = [list(r) for r in table]
+    width = len(table[0]) if table else 0
+    starts, slots, used = [0], [], 0
+    for i, (length, new) in enumerate(zip(lengths, news)):
+        length = min(max(length, 0), width * block)
+        new = min(max(new, 0), length)
+        before = length - new
+        for b in range(-(-before // block), -(-length // block)):
+            table[i][b] = free[used] if used < len(free) else -1
+            used += 1
+        for j in range(before, length):
+            b = table[i][j // block]
+            slots.append(b * block + j % block if b >= 0 else -1)
+        starts.append(starts[-1] + new)
+    slots = (slots + [-1] * n_slots)[:n_slots]
+    return table, starts, slots, used
+
+
+def cache_attention(Q, k, v, k_scale, v_scale, table, lengths, d, block, scale=None, cap=0.0, slopes=None):
+    """(O, bound) in float64 [batch][nq][hq][d] from code values (float64) and scales."""
+    eps = torch.finfo(Q.dtype).eps / 2
+    tiny = 2.0 ** -25 if Q.dtype == torch.float16 else 2.0 ** -134
+    Q = Q.detach().double().cpu()
+    batch, nq, hq, _ = Q.shape
+    hkv = k.shape[1]
+    scale = d ** -0.5 if scale is None else scale
+    O, most = torch.zeros_like(Q), torch.zeros_like(Q)
+    for b in range(batch):
+        length = min(max(lengths[b], 0), len(table[b]) * block)
+        js = [j for j in range(length) if 0 <= table[b][j // block] < k.shape[0]]
+        if not js:
+            most[b] += tiny
+            continue
+        at = torch.tensor([table[b][j // block] for j in js])
+        off = torch.tensor([j % block for j in js])
+        j = torch.tensor(js)
+        p = torch.arange(length - nq, length)[:, None]
+        seen = j[None, :] <= p
+        for h in range(hq):
+            f = h * hkv // hq
+            kk = k[at, f, off, :d] * k_scale[at, f].double()[:, None]
+            vc, vs = v[at, f, :d, off], v_scale[at, f].double()
+            vv = vc * vs[:, None]
+            q = Q[b, :, h]
+            u = scale * q @ kk.T
+            err = STEP32 * (d + 12) * scale * q.abs() @ kk.abs().T
+            s = cap * torch.tanh(u / cap) if cap else u
+            if cap:
+                err = err + 16 * STEP32 * cap
+            if slopes is not None:
+                s = s - float(slopes[h]) * (p - j).abs()
+                err = err + 4 * STEP32 * float(slopes[h]) * (p - j).abs()
+            err = err + 8 * STEP32 * (1 + s.abs())
+            s = s.masked_fill(~seen, -math.inf)
+            P = torch.nan_to_num(torch.softmax(s, 1), nan=0.0)
+            err = 2 * torch.where(seen, err, torch.zeros_like(err)).amax(1, keepdim=True)
+            O[b, :, h] = P @ vv
+            # probabilities in f16, a step of 2^-24 at the least, times the largest scale
+            most[b, :, h] = 1.01 * ((2.0 ** -11 + 2 * err + 4 * STEP32) * (P @ vv.abs()) +
+                                    2.0 ** -25 * float(vs.max()) * (seen.double() @ vc.abs()) + eps * O[b, :, h].abs() + tiny)
+    return O, most

@@ -133,3 +133,86 @@ def test_the_formulas_gradients_against_differences():
             want = float((r[name] * way).sum())
             # step^2 of a third derivative, and 2^-53 of sums of 110 terms over 2e-5
             assert abs((value[0] - value[1]) / (2 * step) - want) < 1e-7 * (1 + abs(want))
+
+
+# ---- the cache ------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("batch,nq,hq,hkv,d,longest", [(1, 1, 8, 1, 128, 200_000), (64, 1, 32, 8, 128, 8192), (0, 1, 1, 1, 64, 100),
+                                                      (4, 3, 8, 4, 64, 512), (1, 1, 1, 1, 1, 0), (1, 1, 1, 1, 8, 1 << 30)])
+def test_cache_plans_stay_under_their_limit(batch, nq, hq, hkv, d, longest):
+    for limit in (0, 10 ** 4, 10 ** 6, GB):
+        p = A.attn_cache_plan(batch, nq, hq, hkv, d, longest, limit)
+        assert p.workspace_bytes <= limit and p.range_tokens % 256 == 0 and p.range_tokens > 0
+        assert p.n_ranges == max(1, -(-longest // p.range_tokens))
+        assert p.workspace_bytes == (up(p.n_ranges * batch * nq * hq * (d + 2) * 4) if p.n_ranges > 1 else 0)
+
+
+def test_cache_shapes_that_are_refused():
+    for shape in [(-1, 1, 1, 1, 8, 5), (1, 0, 1, 1, 8, 5), (1, 1, 3, 2, 8, 5), (1, 1, 1, 1, 0, 5), (1, 1, 1, 1, 8, -1)]:
+        with pytest.raises(A.KnnError) as e:
+            A.attn_cache_plan(*shape, GB)
+        assert e.value.status == A.KNN_ERR_INVALID_ARG
+    for shape in [(1, 1, 1, 1, 129, 5), (1, 1, 1, 1, 8, (1 << 30) + 1), ((1 << 30) + 1, 1, 1, 1, 8, 5), (1, 65536, 1, 1, 8, 5)]:
+        with pytest.raises(A.KnnError) as e:
+            A.attn_cache_plan(*shape, GB)
+        assert e.value.status == A.KNN_ERR_UNSUPPORTED
+    assert [attn._load().attn_cache_row(d) for d in (0, 1, 64, 65, 128, 129, -3)] == [0, 64, 64, 128, 128, 0, 0]
+    assert A.AttnCache.blocks_within(GB, 8, 128, 64) == GB // (8 * (2 * 64 * 128 + 8))
+
+
+def cache(**other):
+    c = attn.CacheStruct(0x1000, 0x1000, 0x1000, 0x1000, 10, 2, 64, 16, 0)
+    for k, v in other.items():
+        setattr(c, k, v)
+    return c
+
+
+def test_cache_calls_that_are_refused():
+    """Refused before anything is launched."""
+    lib, bad = attn._load(), A.KNN_ERR_INVALID_ARG
+    rows, null = attn.RowsStruct(0x1000, 128, 64), attn.RowsStruct(None, 128, 64)
+
+    def append(c=None, dtype=0, k=rows, v=rows, count=3, slots=0x1000):
+        return lib.attn_cache_append(cache() if c is None else c, dtype, k, v, count, slots, None)
+
+    def apply(c=None, dtype=0, q=rows, batch=2, nq=1, hq=4, table=0x1000, width=100, lengths=0x1000, scale=0.1, cap=0.0,
+              limit=GB, ws=0x1000, ws_bytes=1 << 30, out=rows):
+        return lib.attn_cache_apply(cache() if c is None else c, dtype, q, batch, nq, hq, table, width, lengths, scale, cap,
+                                    None, limit, ws, ws_bytes, out, None)
+
+    for other in [dict(k=None), dict(v=None), dict(k_scale=None), dict(v_scale=None), dict(k=0x1008), dict(v=0x1004), dict(blocks=-1),
+                  dict(hkv=0), dict(d=0), dict(d=129), dict(block=8), dict(block=48), dict(block=512), dict(code=2), dict(code=-1)]:
+        assert append(cache(**other)) == bad and apply(cache(**other)) == bad, other
+    assert append(dtype=2) == bad and append(k=null) == bad and append(v=null) == bad and append(count=-1) == bad
+    assert append(slots=None) == bad and lib.attn_cache_append(None, 0, rows, rows, 1, 0x1000, None) == bad
+    assert append(count=1 << 31) == A.KNN_ERR_UNSUPPORTED
+    assert apply(dtype=2) == bad and apply(q=null) == bad and apply(out=null) == bad and apply(table=None) == bad
+    assert apply(lengths=None) == bad and apply(scale=0.0) == bad and apply(scale=float("nan")) == bad and apply(cap=-1.0) == bad
+    assert apply(hq=3) == bad and apply(nq=0) == bad and apply(batch=-1) == bad and apply(width=-1) == bad
+    assert apply(width=1 << 28) == A.KNN_ERR_UNSUPPORTED
+    assert apply(ws=None) == bad and apply(ws=0x1010) == bad and apply(ws_bytes=8) == A.KNN_ERR_WORKSPACE_TOO_SMALL
+
+    def tables(lengths=0x1000, news=0x1000, batch=2, table=0x1000, width=4, block=16, free=0x1000, n_free=3, starts=0x1000,
+               slots=0x1000, n_slots=5, used=0x1000):
+        return lib.attn_cache_map(lengths, news, batch, table, width, block, free, n_free, starts, slots, n_slots, used, None)
+
+    for other in [dict(lengths=None), dict(news=None), dict(table=None), dict(free=None), dict(starts=None), dict(slots=None),
+                  dict(used=None), dict(batch=-1), dict(width=-1), dict(n_free=-1), dict(n_slots=-1), dict(block=0), dict(block=24)]:
+        assert tables(**other) == bad, other
+    assert tables(batch=16385) == A.KNN_ERR_UNSUPPORTED and tables(width=1 << 27) == A.KNN_ERR_UNSUPPORTED
+
+
+def test_the_definition_of_an_append_on_a_case_worked_by_hand():
+    torch = pytest.importorskip("torch")
+    from attn_formulas import append
+
+    k, v = torch.zeros(2, 1, 16, 64, dtype=torch.float64), torch.zeros(2, 1, 64, 16, dtype=torch.float64)
+    s = torch.zeros(2, 1)
+    x = torch.zeros(2, 1, 3, dtype=torch.bfloat16)
+    x[0, 0], x[1, 0] = torch.tensor([127.0, -1.5, 0.5]), torch.tensor([254.0, 3.0, -2.0])
+    k, v, ks, vs = append(k, v, s, s, x[:1], x[:1], [0], 3, 16, "int8")
+    assert ks[0, 0] == 1.0 and k[0, 0, 0, :4].tolist() == [127.0, -2.0, 0.0, 0.0]
+    k, v, ks, vs = append(k, v, ks, vs, x[1:], x[1:], [1], 3, 16, "int8")
+    assert ks[0, 0] == 2.0  # 127 / 2 = 63.5 to 64, -2 / 2 = -1; 3 / 2 to 2
+    assert k[0, 0, :2, :3].tolist() == [[64.0, -1.0, 0.0], [127.0, 2.0, -1.0]]
+    assert v[0, 0, :3, 1].tolist() == [127.0, 2.0, -1.0]
