@@ -62,7 +62,8 @@ attn::Rows rows_of(const attn_rows_t* t, int32_t d) {
     r.data = static_cast<unsigned short*>(t->data);
     r.ld = t->ld;
     r.hs = t->hs;
-    r.wide = reinterpret_cast<uintptr_t>(t->data) % 16 == 0 && d % 8 == 0 && t->ld % 8 == 0 && t->hs % 8 == 0;
+    r.wide = reinterpret_cast<uintptr_t>(t->data) % 16 == 0 && d % 8 == 0 && t->ld % 8 == 0 && t->hs % 8 == 0 &&
+             t->ld < (1 << 22);  // 64 rows are 2^29 bytes at most: offsets in 32 bits
     return r;
 }
 

@@ -234,32 +234,80 @@ __device__ __forceinline__ void stage(unsigned char* lds, const Rows& t, int hea
     }
 }
 
-// First operand, rows as they are: row 32 part + l % 32 of the tile, entries 16 step + 8 (l / 32) ...
-template <int DP>
-__device__ __forceinline__ s16x8 rows_operand(const unsigned char* lds, int part, int step, int lane) {
+// The same without registers in between (t.wide only): 16 bytes a lane, counted by vmcnt; the caller waits with
+// arrive_and_wait.  A lane whose piece lies outside rows or entries reads beyond the descriptor's end, which gives zeros.
+// A thread's piece is the same in every round (THREADS / kPieces is a multiple of the rows that the turn goes by).
+template <int DP, int THREADS>
+struct Direct {
     typedef Tile<DP> L;
-    const int r = lane & 31;
-    const int piece = (2 * step + (lane >> 5)) ^ L::turn(r);
-    return *reinterpret_cast<const s16x8*>(lds + (32 * part + r) * L::kRowBytes + piece * 16);
+    static constexpr int kRows = THREADS / L::kPieces, kRounds = kTileKeys / kRows;
+    static_assert(kRows % L::kPieces == 0, "");
+    uint64_t base;
+    unsigned offset;  // of this thread's piece; behind d: beyond the end
+    int stride;       // of a row, bytes
+    __device__ __forceinline__ Direct(const Rows& t, int head, int d, int tid) {
+        const int r = tid / L::kPieces, piece = (tid % L::kPieces) ^ L::turn(r);
+        base = reinterpret_cast<uint64_t>(t.data + head * t.hs);
+        stride = (int)t.ld * 2;
+        offset = 8 * piece < d ? r * stride + 16 * piece : 0x80000000u;
+    }
+    __device__ __forceinline__ void fetch(const unsigned char* lds, int first, int lo, int hi, int tid) const {
+        const uint64_t from = base + (uint64_t)first * stride;
+        i32x4 words;
+        words[0] = __builtin_amdgcn_readfirstlane((int)from);
+        words[1] = __builtin_amdgcn_readfirstlane((int)(from >> 32) & 0xffff);
+        words[2] = 0x7fffffff;
+        words[3] = 0x00027000;
+        const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)lds;
+        const int row = first + tid / L::kPieces;
+#pragma unroll
+        for (int it = 0; it < kRounds; ++it) {
+            const bool in = row + it * kRows >= lo && row + it * kRows < hi;
+            const unsigned m = __builtin_amdgcn_readfirstlane(at + (it * THREADS + (tid & ~63)) * 16);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(m),
+                         "v"(in ? offset : 0x80000000u), "s"(words), "s"(it * kRows * stride)
+                         : "memory", "m0");
+        }
+    }
+};
+// This wave's loads are in and its reads of LDS done, then all waves'.
+__device__ __forceinline__ void arrive_and_wait() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// First operand, turned: column 32 block + l % 32 of the tile, rows 16 step + 8 e + 4 (l / 32) + b.  The
-// transposing read gives lane i of 16 the i-th of the 16 entries that lanes 4 b .. 4 b + 3 hold, b = 0 .. 3.
+// Where a lane reads its operands, from the tile's start.  (A power of two's worth of pieces a row: the piece's
+// number and the turn meet in an exclusive-or, which takes what is the same for all lanes last.)
 template <int DP>
-__device__ __forceinline__ s16x8 columns_operand(const unsigned char* lds, int block, int step, int lane) {
+struct Lane {
     typedef Tile<DP> L;
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const int b = (lane >> 2) & 3, half = lane >> 5;
-    const int piece = 4 * block + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-    s16x4 part[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int r = 8 * e + 4 * half + b;  // the row's last four bits
-        const unsigned char* p = lds + (16 * step + r) * L::kRowBytes + ((piece ^ L::turn(r)) * 16) + (lane & 1) * 8;
-        part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    unsigned rows, columns;
+    __device__ __forceinline__ explicit Lane(int lane) {
+        const int half = lane >> 5, r = lane & 31;
+        rows = r * L::kRowBytes + (half ^ L::turn(r)) * 16;
+        const int b = (lane >> 2) & 3, c = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+        columns = (4 * half + b) * L::kRowBytes + (c ^ L::turn(4 * half + b)) * 16 + (lane & 1) * 8;
     }
-    return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-}
+    __device__ __forceinline__ void other(unsigned bytes) {  // the tile that many bytes away, a power of two, in either direction
+        rows ^= bytes;
+        columns ^= bytes;
+    }
+    // First operand, rows as they are: row 32 part + l % 32 of the tile, entries 16 step + 8 (l / 32) ...
+    __device__ __forceinline__ s16x8 row(const unsigned char* lds, int part, int step) const {
+        return *reinterpret_cast<const s16x8*>(lds + (rows ^ (32 * step)) + 32 * part * L::kRowBytes);
+    }
+    // First operand, turned: column 32 block + l % 32 of the tile, rows 16 step + 8 e + 4 (l / 32) + b.  The
+    // transposing read gives lane i of 16 the i-th of the 16 entries that lanes 4 b .. 4 b + 3 hold, b = 0 .. 3.
+    __device__ __forceinline__ s16x8 column(const unsigned char* lds, int block, int step) const {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        s16x4 part[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const unsigned char* p = lds + (columns ^ (64 * block ^ (L::turn(8 * e) * 16))) + (16 * step + 8 * e) * L::kRowBytes;
+            part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+        }
+        return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
 
 // Second operand from 16 numbers of a 32 x 32 product: registers 8 step .. 8 step + 7.
 template <typename T>

@@ -63,7 +63,7 @@ template <typename T, int DP>
 __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     typedef Tile<DP> L;
     constexpr int kBlocks = DP / 32, kSteps = DP / 16;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[2 * L::kBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * L::kBytes];
     __shared__ int ends[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int tiles = (p.mask.n + kTileRows - 1) / kTileRows;
@@ -111,19 +111,33 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
         for (int b = 0; b < kBlocks; ++b) sum[b] = f32x16{};
         top = -kInf;
         total = 0.f;
-        for (int s = s0; s < s1; ++s) {
+        // two pairs of buffers: while one is worked on the other is filled
+        const bool direct = p.k.wide && p.v.wide && entries == kAsTheyAre;
+        const Direct<DP, 256> from_k(p.k, kv, p.d, tid), from_v(p.v, kv, p.d, tid);
+        Lane<DP> at(lane);
+        auto fetch = [&](int s) {
+            const unsigned char* const to = lds + (s - s0 & 1) * 2 * L::kBytes;
+            from_k.fetch(to, first + s * kTileKeys, first, last, tid);
+            from_v.fetch(to + L::kBytes, first + s * kTileKeys, first, last, tid);
+        };
+        arrive_and_wait();
+        if (direct && s0 < s1) fetch(s0);
+        for (int s = s0; s < s1; ++s, at.other(2 * L::kBytes)) {
             const int j0 = first + s * kTileKeys;
-            __syncthreads();
-            stage<T, DP, 256>(lds, p.k, kv, j0, first, last, p.d, tid, kAsTheyAre);
-            stage<T, DP, 256>(lds + L::kBytes, p.v, kv, j0, first, last, p.d, tid, entries);
-            __syncthreads();
+            if (!direct) {
+                unsigned char* const to = lds + (s - s0 & 1) * 2 * L::kBytes;
+                stage<T, DP, 256>(to, p.k, kv, j0, first, last, p.d, tid, kAsTheyAre);
+                stage<T, DP, 256>(to + L::kBytes, p.v, kv, j0, first, last, p.d, tid, entries);
+            }
+            arrive_and_wait();
+            if (direct && s + 1 < s1) fetch(s + 1);
             if (j0 >= high || j0 + kTileKeys <= low) continue;
             f32x16 x[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 x[t] = f32x16{};
 #pragma unroll
-                for (int k = 0; k < kSteps; ++k) x[t] = T::mfma(rows_operand<DP>(lds, t, k, lane), q[k], x[t]);
+                for (int k = 0; k < kSteps; ++k) x[t] = T::mfma(at.row(lds, t, k), q[k], x[t]);
             }
             if (p.cap > 0.f) {
 #pragma unroll
@@ -183,7 +197,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    sum[b] = T::mfma(columns_operand<DP>(lds + L::kBytes, b, k, lane), weights[k], sum[b]);
+                    sum[b] = T::mfma(at.column(lds + L::kBytes, b, k), weights[k], sum[b]);
         }
         if (entries == kAsTheyAre) {
             float zero = 0.f;

@@ -85,6 +85,7 @@ __global__ __launch_bounds__(256, DP == 96 ? 1 : 2) void attn_grad_rows_kernel(P
     if (see.inside && half == 0) p.rowsums[at] = rowsum;
     const Scores to(p, head);
 
+    const Lane<DP> at_lane(lane);
     f32x16 sum[kBlocks];
     // An entry of K that is not finite meets the zero weights of rows that do not see it as well.  If a sum comes
     // out not finite the workgroup walks once more with those entries as zeros: the rows that see one have a
@@ -103,8 +104,8 @@ __global__ __launch_bounds__(256, DP == 96 ? 1 : 2) void attn_grad_rows_kernel(P
                 f32x16 x{}, y{};
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) {
-                    x = T::mfma(rows_operand<DP>(lds, t, k, lane), q[k], x);
-                    y = T::mfma(rows_operand<DP>(lds + L::kBytes, t, k, lane), g[k], y);
+                    x = T::mfma(at_lane.row(lds, t, k), q[k], x);
+                    y = T::mfma(at_lane.row(lds + L::kBytes, t, k), g[k], y);
                 }
                 const float away = (float)(see.at - j0 - 4 * half - 32 * t);
 #pragma unroll
@@ -119,8 +120,8 @@ __global__ __launch_bounds__(256, DP == 96 ? 1 : 2) void attn_grad_rows_kernel(P
                 const s16x8 w0 = rounded_operand<T>(x, 0), w1 = rounded_operand<T>(x, 1);
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
-                    sum[b] = T::mfma(columns_operand<DP>(lds, b, 2 * t, lane), w0, sum[b]);
-                    sum[b] = T::mfma(columns_operand<DP>(lds, b, 2 * t + 1, lane), w1, sum[b]);
+                    sum[b] = T::mfma(at_lane.column(lds, b, 2 * t), w0, sum[b]);
+                    sum[b] = T::mfma(at_lane.column(lds, b, 2 * t + 1), w1, sum[b]);
                 }
             }
         }
@@ -185,6 +186,7 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
         v[s] = __builtin_bit_cast(s16x8, b);
     }
 
+    const Lane<DP> at_lane(lane);
     f32x16 dk[kBlocks], dv[kBlocks];
     // As by rows: entries of Q and dO that are not finite as zeros in a second walk, and P as NaN for rows whose
     // row sum is not finite, which dO's and V's make it.
@@ -215,8 +217,8 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
                     f32x16 x{}, y{};
 #pragma unroll
                     for (int c = 0; c < kSteps; ++c) {
-                        x = T::mfma(rows_operand<DP>(lds, t, c, lane), k[c], x);
-                        y = T::mfma(rows_operand<DP>(lds + L::kBytes, t, c, lane), v[c], y);
+                        x = T::mfma(at_lane.row(lds, t, c), k[c], x);
+                        y = T::mfma(at_lane.row(lds + L::kBytes, t, c), v[c], y);
                     }
                     const float away = (float)(i0 + see.at - key + 4 * half + 32 * t);
 #pragma unroll
@@ -241,8 +243,8 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
                         const s16x8 weights = rounded_operand<T>(x, c), slopes = rounded_operand<T>(y, c);
 #pragma unroll
                         for (int b = 0; b < kBlocks; ++b) {
-                            dv[b] = T::mfma(columns_operand<DP>(lds + L::kBytes, b, 2 * t + c, lane), weights, dv[b]);
-                            dk[b] = T::mfma(columns_operand<DP>(lds, b, 2 * t + c, lane), slopes, dk[b]);
+                            dv[b] = T::mfma(at_lane.column(lds + L::kBytes, b, 2 * t + c), weights, dv[b]);
+                            dk[b] = T::mfma(at_lane.column(lds, b, 2 * t + c), slopes, dk[b]);
                         }
                     }
                 }
