@@ -65,8 +65,8 @@ typedef struct {
  * The plan.  One workgroup owns tile_rows rows of one head and walks the keys; where that leaves
  * compute units idle and the limit has room, the keys are cut into n_splits ranges walked
  * concurrently, whose unnormalised sums, maxima and totals (fp32) lie in the workspace until a last
- * kernel joins them in ascending range order.  The gradient keeps one fp32 number per row and head
- * (the row sums of dO * O), and cuts the heads that share a K and V into n_splits parts likewise.
+ * kernel joins them in ascending range order.  The gradient keeps two fp32 numbers per row and head
+ * (the row sums of dO * O, the log-sums), and cuts the heads that share a K and V into n_splits parts likewise.
  * Results differ between limits that give different n_splits by the rounding of those sums.
  */
 typedef struct {

@@ -116,7 +116,7 @@ extern "C" knn_status attn_grad_plan(int64_t n, int64_t m, int32_t hq, int32_t h
                                      attn_plan_t* out) {
     const knn_status st = check_shape(n, m, hq, hkv, d, out);
     if (st != KNN_OK) return st;
-    const uint64_t sums = knn::align_up((uint64_t)n * hq * 4);
+    const uint64_t sums = knn::align_up((uint64_t)n * hq * 8);
     out->min_limit_bytes = sums;
     if (mem_limit_bytes < sums) return KNN_ERR_MEM_LIMIT_TOO_SMALL;
     const int64_t tiles = (m + attn::kTileRows - 1) / attn::kTileRows * hkv;
@@ -191,7 +191,7 @@ extern "C" knn_status attn_grad(const attn_rows_t* Q, const attn_rows_t* K, cons
     p.lse = const_cast<float*>(lse);
     p.splits = plan.n_splits;
     p.rowsums = static_cast<float*>(workspace);
-    p.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + knn::align_up((uint64_t)n * hq * 4));
+    p.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + knn::align_up((uint64_t)n * hq * 8));
     hipEvent_t t = knn::profile_mark(stream);
     const hipError_t e = attn::launch_grad(p, stream);
     if (e != hipSuccess) {

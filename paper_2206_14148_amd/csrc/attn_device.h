@@ -270,6 +270,20 @@ struct Direct {
         }
     }
 };
+// Up to 64 words of one wave likewise; zeros from `count` on.
+__device__ __forceinline__ void fetch_words(const float* lds, const float* from, int lane, int count) {
+    const uint64_t base = reinterpret_cast<uint64_t>(from);
+    i32x4 words;
+    words[0] = __builtin_amdgcn_readfirstlane((int)base);
+    words[1] = __builtin_amdgcn_readfirstlane((int)(base >> 32) & 0xffff);
+    words[2] = 0x7fffffff;
+    words[3] = 0x00027000;
+    const unsigned m =
+        __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) const float*)lds);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(m),
+                 "v"(lane < count ? 4u * lane : 0x80000000u), "s"(words)
+                 : "memory", "m0");
+}
 // This wave's loads are in and its reads of LDS done, then all waves'.
 __device__ __forceinline__ void arrive_and_wait() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");

@@ -39,7 +39,7 @@ template <typename T, int DP>
 __global__ __launch_bounds__(256, DP == 96 ? 1 : 2) void attn_grad_rows_kernel(Problem p) {
     typedef Tile<DP> L;
     constexpr int kBlocks = DP / 32, kSteps = DP / 16;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[2 * L::kBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * L::kBytes];
     __shared__ int ends[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int tiles = (p.mask.n + kTileRows - 1) / kTileRows;
@@ -82,21 +82,35 @@ __global__ __launch_bounds__(256, DP == 96 ? 1 : 2) void attn_grad_rows_kernel(P
     }
     rowsum = sum_of_halves(rowsum);
     const float lse = see.inside ? in_twos(p.lse[at]) : kInf;
-    if (see.inside && half == 0) p.rowsums[at] = rowsum;
+    if (see.inside && half == 0) {  // for the walk by keys, whose entries of Q and dO may stand in as zeros
+        p.rowsums[at] = rowsum;
+        p.rowsums[(int64_t)p.hq * p.mask.n + at] = fabsf(rowsum) < kInf ? lse : __builtin_nanf("");
+    }
     const Scores to(p, head);
 
-    const Lane<DP> at_lane(lane);
     f32x16 sum[kBlocks];
     // An entry of K that is not finite meets the zero weights of rows that do not see it as well.  If a sum comes
     // out not finite the workgroup walks once more with those entries as zeros: the rows that see one have a
     // log-sum that is NaN, and with it P.
     for (int entries = kAsTheyAre;; ++entries) {
         for (int b = 0; b < kBlocks; ++b) sum[b] = f32x16{};
-        for (int j0 = first; j0 < last; j0 += kTileKeys) {
-            __syncthreads();
-            stage<T, DP, 256>(lds, p.k, kv, j0, first, last, p.d, tid, entries);
-            stage<T, DP, 256>(lds + L::kBytes, p.v, kv, j0, first, last, p.d, tid, kAsTheyAre);
-            __syncthreads();
+        const bool direct = p.k.wide && p.v.wide && entries == kAsTheyAre;
+        const Direct<DP, 256> from_k(p.k, kv, p.d, tid), from_v(p.v, kv, p.d, tid);
+        Lane<DP> at_lane(lane);
+        int buffer = 0;
+        auto fetch = [&](int j0, int to) {
+            from_k.fetch(lds + to, j0, first, last, tid);
+            from_v.fetch(lds + to + L::kBytes, j0, first, last, tid);
+        };
+        arrive_and_wait();
+        if (direct && first < last) fetch(first, 0);
+        for (int j0 = first; j0 < last; j0 += kTileKeys, buffer ^= 2 * L::kBytes, at_lane.other(2 * L::kBytes)) {
+            if (!direct) {
+                stage<T, DP, 256>(lds + buffer, p.k, kv, j0, first, last, p.d, tid, entries);
+                stage<T, DP, 256>(lds + buffer + L::kBytes, p.v, kv, j0, first, last, p.d, tid, kAsTheyAre);
+            }
+            arrive_and_wait();
+            if (direct && j0 + kTileKeys < last) fetch(j0 + kTileKeys, buffer ^ 2 * L::kBytes);
             if (j0 >= high || j0 + kTileKeys <= low) continue;
             const bool edge = j0 < all_low || j0 + kTileKeys > all_high;
 #pragma unroll
@@ -150,8 +164,8 @@ template <typename T, int DP>
 __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
     typedef Tile<DP> L;
     constexpr int kBlocks = DP / 32, kSteps = DP / 16;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[2 * L::kBytes];
-    __shared__ __attribute__((aligned(16))) float of_rows[2][kTileKeys];  // log-sums, row sums
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * L::kBytes];
+    __shared__ __attribute__((aligned(16))) float of_rows[2][2][kTileKeys];  // log-sums, row sums
     __shared__ int ends[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int tiles = (p.mask.m + kTileRows - 1) / kTileRows, group = p.hq / p.hkv;
@@ -186,30 +200,46 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
         v[s] = __builtin_bit_cast(s16x8, b);
     }
 
-    const Lane<DP> at_lane(lane);
     f32x16 dk[kBlocks], dv[kBlocks];
-    // As by rows: entries of Q and dO that are not finite as zeros in a second walk, and P as NaN for rows whose
-    // row sum is not finite, which dO's and V's make it.
+    const int64_t all = (int64_t)p.hq * p.mask.n;
+    const int head0 = kv * group + group * part / p.splits, head1 = kv * group + group * (part + 1) / p.splits;
+    // As by rows: entries of Q and dO that are not finite as zeros in a second walk.  Their rows have a log-sum or a
+    // row sum, and with it P, that is NaN.
     for (int entries = kAsTheyAre;; ++entries) {
         for (int b = 0; b < kBlocks; ++b) dk[b] = dv[b] = f32x16{};
-        for (int head = kv * group + group * part / p.splits; head < kv * group + group * (part + 1) / p.splits; ++head) {
+        const bool direct = p.q.wide && p.dO.wide && entries == kAsTheyAre;
+        Lane<DP> at_lane(lane);
+        int buffer = 0;
+        auto fetch = [&](int head, int i0, int to) {
+            const Direct<DP, 256> from_q(p.q, head, p.d, tid), from_g(p.dO, head, p.d, tid);
+            from_q.fetch(lds + to * 2 * L::kBytes, i0, first, last, tid);
+            from_g.fetch(lds + to * 2 * L::kBytes + L::kBytes, i0, first, last, tid);
+            if (wave < 2) {
+                const float* const from = p.rowsums + (wave ? 0 : all) + (int64_t)head * p.mask.n + i0;
+                fetch_words(of_rows[to][wave], from, lane, last - i0);
+            }
+        };
+        arrive_and_wait();
+        if (direct && first < last) fetch(head0, first, 0);
+        for (int head = head0; head < head1; ++head) {
             const Scores to(p, head);
-            for (int i0 = first; i0 < last; i0 += kTileKeys) {
-                __syncthreads();
-                stage<T, DP, 256>(lds, p.q, head, i0, first, last, p.d, tid, entries);
-                stage<T, DP, 256>(lds + L::kBytes, p.dO, head, i0, first, last, p.d, tid, entries);
-                if (tid < kTileKeys) {
-                    float a = kInf, b = 0.f;
-                    if (i0 + tid < last) {
-                        const int64_t at = (int64_t)head * p.mask.n + i0 + tid;
-                        a = in_twos(p.lse[at]);
-                        b = p.rowsums[at];
-                        if (entries != kAsTheyAre && !(fabsf(b) < kInf)) a = b = __builtin_nanf("");
+            for (int i0 = first; i0 < last; i0 += kTileKeys, buffer ^= 1, at_lane.other(2 * L::kBytes)) {
+                if (!direct) {
+                    unsigned char* const to = lds + buffer * 2 * L::kBytes;
+                    stage<T, DP, 256>(to, p.q, head, i0, first, last, p.d, tid, entries);
+                    stage<T, DP, 256>(to + L::kBytes, p.dO, head, i0, first, last, p.d, tid, entries);
+                    if (tid < 2 * kTileKeys) {
+                        const float* const from = p.rowsums + (wave ? 0 : all) + (int64_t)head * p.mask.n + i0;
+                        of_rows[buffer][wave][lane] = i0 + lane < last ? from[lane] : 0.f;
                     }
-                    of_rows[0][tid] = a;
-                    of_rows[1][tid] = b;
                 }
-                __syncthreads();
+                arrive_and_wait();
+                if (direct) {
+                    if (i0 + kTileKeys < last)
+                        fetch(head, i0 + kTileKeys, buffer ^ 1);
+                    else if (head + 1 < head1)
+                        fetch(head + 1, first, buffer ^ 1);
+                }
                 if (i0 >= high || i0 + kTileKeys <= low) continue;
                 const bool edge = i0 < all_low || i0 + kTileKeys > all_high;
 #pragma unroll
@@ -223,8 +253,8 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
                     const float away = (float)(i0 + see.at - key + 4 * half + 32 * t);
 #pragma unroll
                     for (int a = 0; a < 4; ++a) {
-                        const f32x4 lse = *reinterpret_cast<const f32x4*>(&of_rows[0][32 * t + 8 * a + 4 * half]);
-                        const f32x4 rowsum = *reinterpret_cast<const f32x4*>(&of_rows[1][32 * t + 8 * a + 4 * half]);
+                        const f32x4 lse = *reinterpret_cast<const f32x4*>(&of_rows[buffer][0][32 * t + 8 * a + 4 * half]);
+                        const f32x4 rowsum = *reinterpret_cast<const f32x4*>(&of_rows[buffer][1][32 * t + 8 * a + 4 * half]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             float steep = 1.f;
