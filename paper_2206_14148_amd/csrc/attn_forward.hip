@@ -96,21 +96,23 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
         if (see.inside) v = entries8(p.q.data + row * p.q.ld + head * p.q.hs, 16 * s + 8 * half, p.d, p.q.wide);
         q[s] = __builtin_bit_cast(s16x8, v);
     }
-    const bool general = p.cap > 0.f || p.slopes;
-    const float slope = p.slopes ? p.slopes[head] * kLog2e : 0.f;
-    const float factor = general ? 1.f : p.scale * kLog2e;  // of what the loop calls scores, to powers of two
+    // What the walk calls a score is u / scale: the product itself, and a cap and slopes divided by the scale.
+    const float factor = p.scale * kLog2e;  // of a score, to powers of two
+    const bool capped = p.cap > 0.f;
+    const float to_cap = capped ? 2.f * factor / p.cap : 0.f, from_cap = p.cap / p.scale;
+    const float slope = p.slopes ? p.slopes[head] / p.scale : 0.f;
     const float slack = kSlack / factor;
-    const float to_cap = p.cap > 0.f ? 2.f * kLog2e * p.scale / p.cap : 0.f, from_cap = p.cap * kLog2e;
 
     f32x16 sum[kBlocks];
-    float top, total;
+    float top, total;  // of a lane's row: what its scores are taken less of, the sum of its weights (of half the keys)
+    float most_over;   // how far a score may be over top: slack, and for a row that has seen no key nothing at all
     // An infinity or a NaN in V meets the zero weights of rows that do not see it as well, and 0 * infinity is NaN.
     // If any sum comes out not finite the workgroup walks three times more: with those entries as zeros, then with
     // ones for what raises a sum to +infinity and to -infinity, whose sums are not zero for the rows that see one.
     for (int entries = kAsTheyAre;; ++entries) {
         for (int b = 0; b < kBlocks; ++b) sum[b] = f32x16{};
-        top = -kInf;
-        total = 0.f;
+        top = total = 0.f;
+        most_over = -kInf;
         // two pairs of buffers: while one is worked on the other is filled
         const bool direct = p.k.wide && p.v.wide && entries == kAsTheyAre;
         const Direct<DP, 256> from_k(p.k, kv, p.d, tid), from_v(p.v, kv, p.d, tid);
@@ -132,24 +134,23 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
             arrive_and_wait();
             if (direct && s + 1 < s1) fetch(s + 1);
             if (j0 >= high || j0 + kTileKeys <= low) continue;
+            // top comes off as the product's first summand
+            const float less = capped ? 0.f : -top;
             f32x16 x[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                x[t] = f32x16{};
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[t][e] = less;
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) x[t] = T::mfma(at.row(lds, t, k), q[k], x[t]);
             }
-            if (p.cap > 0.f) {
+            if (capped) {
+                const float one = from_cap - top, two = -2.f * from_cap;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        x[t][e] = from_cap * __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * x[t][e])), 1.f);
-            } else if (general) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) x[t][e] *= p.scale * kLog2e;
+                        x[t][e] = __builtin_fmaf(two, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * x[t][e])), one);
             }
             if (p.slopes) {
                 const float away = (float)(see.at - j0 - 4 * half);
@@ -173,21 +174,24 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = fmaxf(most, x[1][e]);
             most = max_of_halves(most);
-            if (__any(most > top + slack)) {
-                const float now = fmaxf(top, most);
-                const float shrink = top == now ? 1.f : __builtin_amdgcn_exp2f((top - now) * factor);
-                top = now;
+            if (__any(most > most_over)) {
+                const bool none = most_over != slack;
+                const float up = none ? (most == -kInf ? 0.f : most) : fmaxf(most, 0.f);
+                const float shrink = none ? 1.f : __builtin_amdgcn_exp2f(-up * factor);
+                if (most > -kInf) most_over = slack;
+                top += up;
                 total *= shrink;
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) sum[b] *= shrink;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) x[t] -= up;
             }
-            const float base = top == -kInf ? 0.f : top;
             s16x8 weights[4];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    x[t][e] = __builtin_amdgcn_exp2f((x[t][e] - base) * factor);  // (the largest: 0, however large)
+                    x[t][e] = __builtin_amdgcn_exp2f(x[t][e] * factor);
                     total += x[t][e];
                 }
                 weights[2 * t] = rounded_operand<T>(x[t], 0);
@@ -207,7 +211,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
                 for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(sum[b][e], 0.f, zero);
             if (__syncthreads_or(zero != 0.f)) continue;  // (NaN)
         }
-        if (see.inside) write_rows<T, kBlocks>(p, see, head, row, split, half, entries, sum, top * factor, sum_of_halves(total));
+        if (see.inside) write_rows<T, kBlocks>(p, see, head, row, split, half, entries, sum, most_over == slack ? top * factor : -kInf, sum_of_halves(total));
         if (entries == kAsTheyAre || entries == kDown) break;
     }
 }
