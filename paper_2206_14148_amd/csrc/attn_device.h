@@ -284,9 +284,13 @@ __device__ __forceinline__ void fetch_words(const float* lds, const float* from,
                  "v"(lane < count ? 4u * lane : 0x80000000u), "s"(words)
                  : "memory", "m0");
 }
-// This wave's loads are in and its reads of LDS done, then all waves'.
+// This wave's loads are in and its reads of LDS done, then all waves'.  (Built-ins, so that the compiler knows what
+// has arrived: it would wait for the loads of the rows again in every round, and with them for the tiles under way.)
 __device__ __forceinline__ void arrive_and_wait() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 // Where a lane reads its operands, from the tile's start.  (A power of two's worth of pieces a row: the piece's
