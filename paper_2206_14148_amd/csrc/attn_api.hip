@@ -19,9 +19,10 @@ namespace {
 
 constexpr int64_t kMostRows = (int64_t)1 << 30;
 
-// Workgroups that fill the GPU: two on a compute unit, and one of the kernel by keys, whose registers
-// are those of two.
-constexpr int64_t kWantRows = 2 * knn::kNumCU, kWantKeys = knn::kNumCU;
+// Workgroups that fill the GPU: two on a compute unit.  Of the kernel by keys one is on a compute unit at a time, its
+// registers are those of two; with a causal mask the first keys' are twice as long as the mean, so that four rounds of
+// shorter ones end sooner than one of long ones, although the parts have to be written and read.
+constexpr int64_t kWantRows = 2 * knn::kNumCU, kWantKeys = 4 * knn::kNumCU;
 // A range of keys is worth a workgroup of its own from this many on: its sums are written and read once more, 4 d bytes a
 // row each way, against 4 d bytes a key read.
 constexpr int64_t kLeastRange = 256;
@@ -36,7 +37,7 @@ knn_status check_shape(int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t d,
     if (n < 0 || m < 0 || hkv < 1 || hq < hkv || hq % hkv != 0 || d < 1) return KNN_ERR_INVALID_ARG;
     if (d > ATTN_MAX_D || n > kMostRows || m > kMostRows || hq > 65535) return KNN_ERR_UNSUPPORTED;
     // one workgroup for each tile and head, at most 64 ranges each
-    if ((n / attn::kTileRows + 1) * hq > (1 << 24) || (m / attn::kTileRows + 1) * hq > (1 << 24)) return KNN_ERR_UNSUPPORTED;
+    if ((n / attn::kTileRows + 1) * hq > (1 << 23) || (m / attn::kTileRows + 1) * hq > (1 << 23)) return KNN_ERR_UNSUPPORTED;
     out->n = n;
     out->m = m;
     out->hq = hq;
@@ -102,7 +103,7 @@ extern "C" knn_status attn_plan(int64_t n, int64_t m, int32_t hq, int32_t hkv, i
                                 attn_plan_t* out) {
     const knn_status st = check_shape(n, m, hq, hkv, d, out);
     if (st != KNN_OK) return st;
-    const int64_t tiles = (n + attn::kTileRows - 1) / attn::kTileRows * hq;
+    const int64_t tiles = (n * (hq / hkv) + attn::kTileRows - 1) / attn::kTileRows * hkv;
     int64_t s = 1;
     while (tiles > 0 && tiles * s < kWantRows && 2 * s <= attn::kMaxSplits && m / (2 * s) >= kLeastRange &&
            part_bytes(n, hq, d, 2 * s) <= mem_limit_bytes)

@@ -448,17 +448,8 @@ __global__ __launch_bounds__(256) void attn_cache_join_kernel(CacheProblem p) {
     const int row = (int)(at % rows), head = (int)(at / rows % c.hkv), b = (int)(at / rows / c.hkv);
     const int length = min(max(p.lengths[b], 0), p.width * c.block);
     const int ranges = max(1, (length + p.range_tokens - 1) / p.range_tokens);
-    const float* const ends_of = p.partial + p.ranges * all * c.d;
-    float top = -kInf;
-    for (int s = 0; s < ranges; ++s) top = fmaxf(top, ends_of[2 * (s * all + at)]);
-    const float base = top == -kInf ? 0.f : top;
-    float total = 0.f, x[2] = {0.f, 0.f};
-    for (int s = 0; s < ranges; ++s) {
-        const float f = __builtin_amdgcn_exp2f(ends_of[2 * (s * all + at)] - base);
-        total = __builtin_fmaf(ends_of[2 * (s * all + at) + 1], f, total);
-        for (int e = 0; e < 2; ++e)
-            if (64 * e + lane < c.d) x[e] = __builtin_fmaf(p.partial[(s * all + at) * c.d + 64 * e + lane], f, x[e]);
-    }
+    float x[2];
+    const float total = join_ranges(p.partial, p.ranges, ranges, all, at, c.d, lane, x).y;
     unsigned short* const o = p.o.data + ((int64_t)b * p.nq + row / group) * p.o.ld + (head * group + row % group) * p.o.hs;
     for (int e = 0; e < 2; ++e)
         if (64 * e + lane < c.d) o[64 * e + lane] = (unsigned short)T::pack(total == 0.f ? 0.f : x[e] / total, 0.f);

@@ -221,7 +221,7 @@ __device__ __forceinline__ void stage(unsigned char* lds, const Rows& t, int hea
                                       int entries) {
     typedef Tile<DP> L;
     const unsigned short* base = t.data + head * t.hs;
-#pragma unroll
+#pragma unroll 1  // (registers)
     for (int it = 0; it < kTileKeys * L::kPieces / THREADS; ++it) {
         const int at = it * THREADS + tid, r = at / L::kPieces, piece = (at % L::kPieces) ^ L::turn(r);
         const int row = first + r;
@@ -354,6 +354,40 @@ __device__ __forceinline__ void put4(unsigned short* p, int c, int d, int wide, 
         if (c + 2 < d) p[c + 2] = (unsigned short)b;
         if (c + 3 < d) p[c + 3] = (unsigned short)(b >> 16);
     }
+}
+
+// The sums of one row over ranges of its keys: partial [ranges][rows][d], behind it [ranges][rows] maximum (in powers of two)
+// and total.  x: entries lane and 64 + lane; returns maximum (0 if there is none) and total.  One wave, at most 64 ranges
+// of which the first `used` hold something.
+__device__ __forceinline__ float2 join_ranges(const float* partial, int ranges, int used, int64_t rows, int64_t at, int d, int lane,
+                                              float* x) {
+    const float* const ends = partial + ranges * rows * d;
+    float top = -kInf, total = 0.f;
+    if (lane < used) {
+        const float2 e = *reinterpret_cast<const float2*>(ends + 2 * (lane * rows + at));
+        top = e.x;
+        total = e.y;
+    }
+    float most = top;
+#pragma unroll
+    for (int s = 32; s; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+    if (most == -kInf) most = 0.f;
+    const float f = __builtin_amdgcn_exp2f(top - most);
+    total *= f;
+    x[0] = x[1] = 0.f;
+    float all = 0.f;
+    const float* o = partial + at * d + lane;
+    const bool in0 = lane < d, in1 = 64 + lane < d;
+#pragma unroll 8
+    for (int s = 0; s < used; ++s, o += rows * d) {
+        const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
+        const float a = in0 ? o[0] : 0.f, b = in1 ? o[64] : 0.f;
+        all += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(total), s));
+        // (zero times an infinity, of a range whose weights have vanished against another's: nothing)
+        x[0] = __builtin_fmaf(fs != 0.f ? a : 0.f, fs, x[0]);
+        x[1] = __builtin_fmaf(fs != 0.f ? b : 0.f, fs, x[1]);
+    }
+    return float2{most, all};
 }
 
 }  // namespace

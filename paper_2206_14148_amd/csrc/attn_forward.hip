@@ -66,12 +66,12 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     __shared__ __attribute__((aligned(16))) unsigned char lds[4 * L::kBytes];
     __shared__ int ends[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-    const int tiles = (p.mask.n + kTileRows - 1) / kTileRows;
+    // The heads that share a K and V stand side by side: "rows" of the tile are rows and, within a row, its heads.
+    const int group = p.hq / p.hkv, tiles = (int)(((int64_t)p.mask.n * group + kTileRows - 1) / kTileRows);
     const int w = work_of(blockIdx.x, gridDim.x);
     // the last rows first: with a causal mask they see the most keys
-    const int split = w % p.splits, tile = tiles - 1 - w / p.splits % tiles, head = w / p.splits / tiles;
-    const int kv = head / (p.hq / p.hkv);
-    const int row = tile * kTileRows + wave * 32 + (lane & 31);
+    const int split = w % p.splits, tile = tiles - 1 - w / p.splits % tiles, kv = w / p.splits / tiles;
+    const int line = tile * kTileRows + wave * 32 + (lane & 31), row = line / group, head = kv * group + line % group;
     const Span see = keys_of_row(p.mask, row);
     const bool some = see.lo < see.hi;
     const int low = wave_least(some ? see.lo : INT_MAX), high = wave_most(some ? see.hi : INT_MIN);
@@ -100,123 +100,155 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     const float factor = p.scale * kLog2e;  // of a score, to powers of two
     const bool capped = p.cap > 0.f;
     const float to_cap = capped ? 2.f * factor / p.cap : 0.f, from_cap = p.cap / p.scale;
-    const float slope = p.slopes ? p.slopes[head] / p.scale : 0.f;
+    const float slope = p.slopes && see.inside ? p.slopes[head] / p.scale : 0.f;
     const float slack = kSlack / factor;
 
     f32x16 sum[kBlocks];
     float top, total;  // of a lane's row: what its scores are taken less of, the sum of its weights (of half the keys)
     float most_over;   // how far a score may be over top: slack, and for a row that has seen no key nothing at all
-    // An infinity or a NaN in V meets the zero weights of rows that do not see it as well, and 0 * infinity is NaN.
-    // If any sum comes out not finite the workgroup walks three times more: with those entries as zeros, then with
-    // ones for what raises a sum to +infinity and to -infinity, whose sums are not zero for the rows that see one.
-    for (int entries = kAsTheyAre;; ++entries) {
+    Lane<DP> at(lane);
+    unsigned char* const keys = lds;
+    unsigned char* const values = lds + 2 * L::kBytes;
+    auto begin = [&]() {
         for (int b = 0; b < kBlocks; ++b) sum[b] = f32x16{};
         top = total = 0.f;
         most_over = -kInf;
-        // two pairs of buffers: while one is worked on the other is filled
-        const bool direct = p.k.wide && p.v.wide && entries == kAsTheyAre;
+    };
+    auto products = [&](f32x16* x) {
+        const float less = capped ? 0.f : -top;  // top comes off as the product's first summand
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[t][e] = less;
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) x[t] = T::mfma(at.row(keys, t, k), q[k], x[t]);
+        }
+    };
+    // A tile's products x to what the weights are the exponentials of.
+    auto scores = [&](f32x16* x, int j0) {
+        if (capped) {
+            const float one = from_cap - top, two = -2.f * from_cap;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    x[t][e] = __builtin_fmaf(two, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * x[t][e])), one);
+        }
+        if (p.slopes) {
+            const float away = (float)(see.at - j0 - 4 * half);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    x[t][e] = __builtin_fmaf(-slope, fabsf(away - (float)(32 * t + 8 * (e >> 2) + (e & 3))), x[t][e]);
+        }
+        if (j0 < all_low || j0 + kTileKeys > all_high) {
+            const unsigned width = (unsigned)(see.hi - see.lo);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if ((unsigned)(j0 + 4 * half + 32 * t + 8 * (e >> 2) + (e & 3) - see.lo) >= width) x[t][e] = -kInf;
+        }
+        float most = x[0][0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) most = fmaxf(most, x[0][e]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) most = fmaxf(most, x[1][e]);
+        most = max_of_halves(most);
+        if (__any(most > most_over)) {
+            const bool none = most_over != slack;
+            const float up = none ? (most == -kInf ? 0.f : most) : fmaxf(most, 0.f);
+            const float shrink = none ? 1.f : __builtin_amdgcn_exp2f(-up * factor);
+            if (most > -kInf) most_over = slack;
+            top += up;
+            total *= shrink;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) sum[b] *= shrink;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) x[t] -= up;
+        }
+    };
+    // One tile that lies in LDS.
+    auto tile_of = [&](int j0) {
+        if (j0 >= high || j0 + kTileKeys <= low) return;
+        f32x16 x[2];
+        products(x);
+        scores(x, j0);
+        s16x8 weights[4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                x[t][e] = __builtin_amdgcn_exp2f(x[t][e] * factor);
+                total += x[t][e];
+            }
+            weights[2 * t] = rounded_operand<T>(x[t], 0);
+            weights[2 * t + 1] = rounded_operand<T>(x[t], 1);
+        }
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[b] = T::mfma(at.column(values, b, k), weights[k], sum[b]);
+    };
+    auto write = [&](int entries) {
+        if (see.inside)
+            write_rows<T, kBlocks>(p, see, head, row, split, half, entries, sum, most_over == slack ? top * factor : -kInf,
+                                   sum_of_halves(total));
+    };
+
+    int entries = kAsTheyAre;
+    auto all_finite = [&]() {
+        float zero = 0.f;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(sum[b][e], 0.f, zero);
+        return !__syncthreads_or(zero != 0.f);  // (NaN)
+    };
+    if (p.k.wide && p.v.wide) {
+        // one pair of buffers is worked on while the other is filled
         const Direct<DP, 256> from_k(p.k, kv, p.d, tid), from_v(p.v, kv, p.d, tid);
-        Lane<DP> at(lane);
-        auto fetch = [&](int s) {
-            const unsigned char* const to = lds + (s - s0 & 1) * 2 * L::kBytes;
-            from_k.fetch(to, first + s * kTileKeys, first, last, tid);
-            from_v.fetch(to + L::kBytes, first + s * kTileKeys, first, last, tid);
+        auto bring = [&](int s) {
+            from_k.fetch(keys + (s - s0 & 1) * L::kBytes, first + s * kTileKeys, first, last, tid);
+            from_v.fetch(values + (s - s0 & 1) * L::kBytes, first + s * kTileKeys, first, last, tid);
         };
-        arrive_and_wait();
-        if (direct && s0 < s1) fetch(s0);
-        for (int s = s0; s < s1; ++s, at.other(2 * L::kBytes)) {
-            const int j0 = first + s * kTileKeys;
-            if (!direct) {
-                unsigned char* const to = lds + (s - s0 & 1) * 2 * L::kBytes;
-                stage<T, DP, 256>(to, p.k, kv, j0, first, last, p.d, tid, kAsTheyAre);
-                stage<T, DP, 256>(to + L::kBytes, p.v, kv, j0, first, last, p.d, tid, entries);
-            }
+        begin();
+        if (s0 < s1) bring(s0);
+        for (int s = s0; s < s1; ++s, at.other(L::kBytes)) {
             arrive_and_wait();
-            if (direct && s + 1 < s1) fetch(s + 1);
-            if (j0 >= high || j0 + kTileKeys <= low) continue;
-            // top comes off as the product's first summand
-            const float less = capped ? 0.f : -top;
-            f32x16 x[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[t][e] = less;
-#pragma unroll
-                for (int k = 0; k < kSteps; ++k) x[t] = T::mfma(at.row(lds, t, k), q[k], x[t]);
-            }
-            if (capped) {
-                const float one = from_cap - top, two = -2.f * from_cap;
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        x[t][e] = __builtin_fmaf(two, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * x[t][e])), one);
-            }
-            if (p.slopes) {
-                const float away = (float)(see.at - j0 - 4 * half);
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        x[t][e] = __builtin_fmaf(-slope, fabsf(away - (float)(32 * t + 8 * (e >> 2) + (e & 3))), x[t][e]);
-            }
-            if (j0 < all_low || j0 + kTileKeys > all_high) {
-                const unsigned width = (unsigned)(see.hi - see.lo);
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if ((unsigned)(j0 + 4 * half + 32 * t + 8 * (e >> 2) + (e & 3) - see.lo) >= width) x[t][e] = -kInf;
-            }
-            float most = x[0][0];
-#pragma unroll
-            for (int e = 1; e < 16; ++e) most = fmaxf(most, x[0][e]);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) most = fmaxf(most, x[1][e]);
-            most = max_of_halves(most);
-            if (__any(most > most_over)) {
-                const bool none = most_over != slack;
-                const float up = none ? (most == -kInf ? 0.f : most) : fmaxf(most, 0.f);
-                const float shrink = none ? 1.f : __builtin_amdgcn_exp2f(-up * factor);
-                if (most > -kInf) most_over = slack;
-                top += up;
-                total *= shrink;
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) sum[b] *= shrink;
-#pragma unroll
-                for (int t = 0; t < 2; ++t) x[t] -= up;
-            }
-            s16x8 weights[4];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    x[t][e] = __builtin_amdgcn_exp2f(x[t][e] * factor);
-                    total += x[t][e];
-                }
-                weights[2 * t] = rounded_operand<T>(x[t], 0);
-                weights[2 * t + 1] = rounded_operand<T>(x[t], 1);
-            }
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    sum[b] = T::mfma(at.column(lds + L::kBytes, b, k), weights[k], sum[b]);
+            if (s + 1 < s1) bring(s + 1);
+            tile_of(first + s * kTileKeys);
         }
-        if (entries == kAsTheyAre) {
-            float zero = 0.f;
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(sum[b][e], 0.f, zero);
-            if (__syncthreads_or(zero != 0.f)) continue;  // (NaN)
+        if (all_finite()) {
+            write(entries);
+            return;
         }
-        if (see.inside) write_rows<T, kBlocks>(p, see, head, row, split, half, entries, sum, most_over == slack ? top * factor : -kInf, sum_of_halves(total));
-        if (entries == kAsTheyAre || entries == kDown) break;
+        at = Lane<DP>(lane);
+        entries = kFinite;
+    }
+    // Without 16-byte reads; and where a sum came out not finite.  An infinity or a NaN in V meets the zero weights of
+    // rows that do not see it as well, and 0 * infinity is NaN.  Then the workgroup walks three times more: with those
+    // entries as zeros, and with ones for what raises a sum to +infinity and to -infinity, whose sums are not zero
+    // for the rows that see one.
+    for (;; ++entries) {
+        begin();
+        for (int s = s0; s < s1; ++s) {
+            const int j0 = first + s * kTileKeys;
+            arrive_and_wait();
+            stage<T, DP, 256>(keys, p.k, kv, j0, first, last, p.d, tid, kAsTheyAre);
+            stage<T, DP, 256>(values, p.v, kv, j0, first, last, p.d, tid, entries);
+            arrive_and_wait();
+            tile_of(j0);
+        }
+        if (entries == kAsTheyAre && !all_finite()) continue;
+        write(entries);
+        if (entries == kAsTheyAre || entries == kDown) return;
     }
 }
 
-// The ranges' sums of one row, in ascending order: a wave for each row and head.
+// The ranges' sums of one row, in ascending order: a wave for each row and head.  Lane s looks after range s.
+static_assert(kMaxSplits <= 64, "");
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_kernel(Problem p) {
     const int lane = threadIdx.x & 63;
@@ -224,30 +256,21 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Problem p) {
     if (at >= rows) return;
     const int head = (int)(at / p.mask.n), row = (int)(at % p.mask.n);
     if (!keys_of_row(p.mask, row).inside) return;
-    const float* ends_of = p.partial + (int64_t)p.splits * rows * p.d;
-    float top = -kInf;
-    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, ends_of[2 * (s * rows + at)]);
-    const float base = top == -kInf ? 0.f : top;
-    float total = 0.f, x[2] = {0.f, 0.f};
-    for (int s = 0; s < p.splits; ++s) {
-        const float f = __builtin_amdgcn_exp2f(ends_of[2 * (s * rows + at)] - base);
-        total = __builtin_fmaf(ends_of[2 * (s * rows + at) + 1], f, total);
-        const float* o = p.partial + (s * rows + at) * p.d;
-        for (int e = 0; e < 2; ++e)
-            if (64 * e + lane < p.d && f != 0.f) x[e] = __builtin_fmaf(o[64 * e + lane], f, x[e]);
-    }
+    float x[2];
+    const float2 ends = join_ranges(p.partial, p.splits, p.splits, rows, at, p.d, lane, x);
+    const float top = ends.x, total = ends.y;
     const float inverse = total == 0.f ? 0.f : 1.f / total;
     for (int e = 0; e < 2; ++e)
         if (64 * e + lane < p.d)
             p.o.data[row * p.o.ld + head * p.o.hs + 64 * e + lane] =
                 (unsigned short)T::pack(total == 0.f ? 0.f : x[e] * inverse, 0.f);
-    if (p.lse && lane == 0) p.lse[at] = total == 0.f ? -kInf : (base + __builtin_amdgcn_logf(total)) * kLn2;
+    if (p.lse && lane == 0) p.lse[at] = total == 0.f ? -kInf : (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 template <typename T>
 hipError_t launch(const Problem& p, hipStream_t stream) {
-    const int64_t tiles = (p.mask.n + kTileRows - 1) / kTileRows;
-    const dim3 grid((unsigned)(tiles * p.hq * p.splits)), block(256);
+    const int64_t tiles = ((int64_t)p.mask.n * (p.hq / p.hkv) + kTileRows - 1) / kTileRows;
+    const dim3 grid((unsigned)(tiles * p.hkv * p.splits)), block(256);
     if (p.d <= 64)
         attn_forward_kernel<T, 64><<<grid, block, 0, stream>>>(p);
     else if (p.d <= 96)

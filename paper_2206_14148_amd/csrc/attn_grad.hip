@@ -8,44 +8,64 @@ namespace attn {
 
 namespace {
 
-// Scores of a tile to P (given the rows' or the row's log-sum, in powers of two) and, where they are capped, to
-// the slope of the cap.
+// 16 products x = <Q, K> and y = <dO, V> of a tile to P and P (y - rowsum) (1 - tanh^2).  What differs between
+// calls (a cap, slopes) is asked once for the 16 and not for each; `lse` and `rowsum` give number e's log-sum, in powers
+// of two, and row sum, `far` how far its row stands from its key.
 struct Scores {
     float factor, to_cap, from_cap, slope;
-    bool capped, general;
+    bool capped, sloped;
     __device__ __forceinline__ Scores(const Problem& p, int head) {
         capped = p.cap > 0.f;
-        general = capped || p.slopes;
-        slope = p.slopes ? p.slopes[head] * kLog2e : 0.f;
+        sloped = p.slopes;
+        slope = sloped ? p.slopes[head] * kLog2e : 0.f;
         factor = p.scale * kLog2e;
         to_cap = capped ? 2.f * kLog2e * p.scale / p.cap : 0.f;
         from_cap = p.cap * kLog2e;
     }
-    // u -> score in powers of two; `steep`: 1 - tanh^2
-    __device__ __forceinline__ float score(float u, float away, float& steep) const {
-        float s = u * factor;
+    __device__ __forceinline__ float tanh_of(float u) const {
+        return __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * u)), 1.f);
+    }
+    template <typename Lse, typename Sum, typename Far>
+    __device__ __forceinline__ void weights(f32x16& x, f32x16& y, Lse lse, Sum rowsum, Far far) const {
+        float by = factor;
         if (capped) {
-            const float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * u)), 1.f);
-            s = from_cap * t;
-            steep = __builtin_fmaf(-t, t, 1.f);
+            by = from_cap;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                x[e] = tanh_of(x[e]);
+                y[e] = (y[e] - rowsum(e)) * __builtin_fmaf(-x[e], x[e], 1.f);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] -= rowsum(e);
         }
-        return __builtin_fmaf(-slope, fabsf(away), s);
+        if (sloped) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(-slope, fabsf(far(e)), by * x[e]);
+            by = 1.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], by, -lse(e)));
+            y[e] *= x[e];
+        }
     }
 };
 
 __device__ __forceinline__ float in_twos(float lse) { return lse == -kInf ? kInf : lse * kLog2e; }  // no keys: P = 0
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256, DP == 96 ? 1 : 2) void attn_grad_rows_kernel(Problem p) {
+__global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     typedef Tile<DP> L;
     constexpr int kBlocks = DP / 32, kSteps = DP / 16;
     __shared__ __attribute__((aligned(16))) unsigned char lds[4 * L::kBytes];
     __shared__ int ends[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-    const int tiles = (p.mask.n + kTileRows - 1) / kTileRows;
+    // (rows and, within a row, the heads that share a K and V, as in the forward pass)
+    const int group = p.hq / p.hkv, tiles = (int)(((int64_t)p.mask.n * group + kTileRows - 1) / kTileRows);
     const int w = work_of(blockIdx.x, gridDim.x);
-    const int tile = tiles - 1 - w % tiles, head = w / tiles, kv = head / (p.hq / p.hkv);
-    const int row = tile * kTileRows + wave * 32 + (lane & 31);
+    const int tile = tiles - 1 - w % tiles, kv = w / tiles;
+    const int line = tile * kTileRows + wave * 32 + (lane & 31), row = line / group, head = kv * group + line % group;
     const Span see = keys_of_row(p.mask, row);
     const bool some = see.lo < see.hi;
     const int low = wave_least(some ? see.lo : INT_MAX), high = wave_most(some ? see.hi : INT_MIN);
@@ -89,63 +109,83 @@ __global__ __launch_bounds__(256, DP == 96 ? 1 : 2) void attn_grad_rows_kernel(P
     const Scores to(p, head);
 
     f32x16 sum[kBlocks];
-    // An entry of K that is not finite meets the zero weights of rows that do not see it as well.  If a sum comes
-    // out not finite the workgroup walks once more with those entries as zeros: the rows that see one have a
-    // log-sum that is NaN, and with it P.
-    for (int entries = kAsTheyAre;; ++entries) {
+    Lane<DP> at_lane(lane);
+    unsigned char* const keys = lds;
+    unsigned char* const values = lds + 2 * L::kBytes;
+    auto begin = [&]() {
         for (int b = 0; b < kBlocks; ++b) sum[b] = f32x16{};
-        const bool direct = p.k.wide && p.v.wide && entries == kAsTheyAre;
-        const Direct<DP, 256> from_k(p.k, kv, p.d, tid), from_v(p.v, kv, p.d, tid);
-        Lane<DP> at_lane(lane);
-        int buffer = 0;
-        auto fetch = [&](int j0, int to) {
-            from_k.fetch(lds + to, j0, first, last, tid);
-            from_v.fetch(lds + to + L::kBytes, j0, first, last, tid);
-        };
-        arrive_and_wait();
-        if (direct && first < last) fetch(first, 0);
-        for (int j0 = first; j0 < last; j0 += kTileKeys, buffer ^= 2 * L::kBytes, at_lane.other(2 * L::kBytes)) {
-            if (!direct) {
-                stage<T, DP, 256>(lds + buffer, p.k, kv, j0, first, last, p.d, tid, entries);
-                stage<T, DP, 256>(lds + buffer + L::kBytes, p.v, kv, j0, first, last, p.d, tid, kAsTheyAre);
+    };
+    // One tile that lies in LDS.
+    auto tile_of = [&](int j0) {
+        if (j0 >= high || j0 + kTileKeys <= low) return;
+        const bool edge = j0 < all_low || j0 + kTileKeys > all_high;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            f32x16 x{}, y{};
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                x = T::mfma(at_lane.row(keys, t, k), q[k], x);
+                y = T::mfma(at_lane.row(values, t, k), g[k], y);
             }
-            arrive_and_wait();
-            if (direct && j0 + kTileKeys < last) fetch(j0 + kTileKeys, buffer ^ 2 * L::kBytes);
-            if (j0 >= high || j0 + kTileKeys <= low) continue;
-            const bool edge = j0 < all_low || j0 + kTileKeys > all_high;
+            const float away = (float)(see.at - j0 - 4 * half - 32 * t);
+            to.weights(x, y, [&](int) { return lse; }, [&](int) { return rowsum; },
+                       [&](int e) { return away - (float)(8 * (e >> 2) + (e & 3)); });
+            if (edge) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                f32x16 x{}, y{};
-#pragma unroll
-                for (int k = 0; k < kSteps; ++k) {
-                    x = T::mfma(at_lane.row(lds, t, k), q[k], x);
-                    y = T::mfma(at_lane.row(lds + L::kBytes, t, k), g[k], y);
-                }
-                const float away = (float)(see.at - j0 - 4 * half - 32 * t);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float steep = 1.f;
-                    const int j = 8 * (e >> 2) + (e & 3);
-                    const float s = to.score(x[e], away - (float)j, steep);
-                    float weight = __builtin_amdgcn_exp2f(s - lse) * (y[e] - rowsum) * steep;
-                    if (edge && (unsigned)(j0 + 4 * half + 32 * t + j - see.lo) >= (unsigned)(see.hi - see.lo)) weight = 0.f;
-                    x[e] = weight;
-                }
-                const s16x8 w0 = rounded_operand<T>(x, 0), w1 = rounded_operand<T>(x, 1);
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    sum[b] = T::mfma(at_lane.column(lds, b, 2 * t), w0, sum[b]);
-                    sum[b] = T::mfma(at_lane.column(lds, b, 2 * t + 1), w1, sum[b]);
-                }
+                for (int e = 0; e < 16; ++e)
+                    if ((unsigned)(j0 + 4 * half + 32 * t + 8 * (e >> 2) + (e & 3) - see.lo) >= (unsigned)(see.hi - see.lo))
+                        y[e] = 0.f;
             }
+            const s16x8 w0 = rounded_operand<T>(y, 0), w1 = rounded_operand<T>(y, 1);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                sum[b] = T::mfma(at_lane.column(keys, b, 2 * t), w0, sum[b]);
+                sum[b] = T::mfma(at_lane.column(keys, b, 2 * t + 1), w1, sum[b]);
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (the halves do not mix: registers)
         }
-        if (entries != kAsTheyAre) break;
+    };
+    auto all_finite = [&]() {
         float zero = 0.f;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(sum[b][e], 0.f, zero);
-        if (!__syncthreads_or(zero != 0.f)) break;
+        return !__syncthreads_or(zero != 0.f);  // (NaN)
+    };
+    int entries = kAsTheyAre;
+    bool done = false;
+    if (p.k.wide && p.v.wide) {
+        const Direct<DP, 256> from_k(p.k, kv, p.d, tid), from_v(p.v, kv, p.d, tid);
+        int buffer = 0;
+        auto bring = [&](int j0, int to) {
+            from_k.fetch(keys + to, j0, first, last, tid);
+            from_v.fetch(values + to, j0, first, last, tid);
+        };
+        begin();
+        if (first < last) bring(first, 0);
+        for (int j0 = first; j0 < last; j0 += kTileKeys, buffer ^= L::kBytes, at_lane.other(L::kBytes)) {
+            arrive_and_wait();
+            if (j0 + kTileKeys < last) bring(j0 + kTileKeys, buffer ^ L::kBytes);
+            tile_of(j0);
+        }
+        done = all_finite();
+        at_lane = Lane<DP>(lane);
+        entries = kFinite;
+    }
+    // Without 16-byte reads; and where a sum came out not finite.  An entry of K that is not finite meets the zero weights
+    // of rows that do not see it as well.  Then the workgroup walks once more with those entries as zeros: the rows that
+    // see one have a log-sum that is NaN, and with it P.
+    for (; !done; ++entries) {
+        begin();
+        for (int j0 = first; j0 < last; j0 += kTileKeys) {
+            arrive_and_wait();
+            stage<T, DP, 256>(keys, p.k, kv, j0, first, last, p.d, tid, entries);
+            stage<T, DP, 256>(values, p.v, kv, j0, first, last, p.d, tid, kAsTheyAre);
+            arrive_and_wait();
+            tile_of(j0);
+        }
+        done = entries == kFinite || all_finite();
     }
     if (!see.inside) return;
     unsigned short* const o = p.dq.data + row * p.dq.ld + head * p.dq.hs;
@@ -201,92 +241,164 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
     }
 
     f32x16 dk[kBlocks], dv[kBlocks];
+    Lane<DP> at_lane(lane);
+    unsigned char* const queries = lds;
+    unsigned char* const grads = lds + 2 * L::kBytes;
     const int64_t all = (int64_t)p.hq * p.mask.n;
     const int head0 = kv * group + group * part / p.splits, head1 = kv * group + group * (part + 1) / p.splits;
-    // As by rows: entries of Q and dO that are not finite as zeros in a second walk.  Their rows have a log-sum or a
-    // row sum, and with it P, that is NaN.
-    for (int entries = kAsTheyAre;; ++entries) {
+    auto begin = [&]() {
         for (int b = 0; b < kBlocks; ++b) dk[b] = dv[b] = f32x16{};
-        const bool direct = p.q.wide && p.dO.wide && entries == kAsTheyAre;
-        Lane<DP> at_lane(lane);
-        int buffer = 0;
-        auto fetch = [&](int head, int i0, int to) {
-            const Direct<DP, 256> from_q(p.q, head, p.d, tid), from_g(p.dO, head, p.d, tid);
-            from_q.fetch(lds + to * 2 * L::kBytes, i0, first, last, tid);
-            from_g.fetch(lds + to * 2 * L::kBytes + L::kBytes, i0, first, last, tid);
-            if (wave < 2) {
-                const float* const from = p.rowsums + (wave ? 0 : all) + (int64_t)head * p.mask.n + i0;
-                fetch_words(of_rows[to][wave], from, lane, last - i0);
-            }
+    };
+    // One tile of rows that lies in LDS, 32 rows at a time: 4 products of kSteps instructions each, in the order written
+    // here.  A wave has its SIMD to itself (the accumulators alone are half of what two could have), so what would wait has to
+    // be begun early: every operand is read kAhead instructions before its own, the exponentials stand among the
+    // products of dO and V, and the rest among the sums for dV.
+    auto tile_of = [&](const Scores& to, int i0, int buffer) {
+        if (i0 >= high || i0 + kTileKeys <= low) return;
+        constexpr int kAhead = 4, kAll = 2 * kSteps + 4 * kBlocks, kEach = (16 + kSteps - 1) / kSteps;
+        const bool edge = i0 < all_low || i0 + kTileKeys > all_high;
+        auto operand = [&](int i) {
+            const int t = i / kAll, j = i % kAll, c = j - 2 * kSteps;
+            if (j < kSteps) return at_lane.row(queries, t, j);
+            if (j < 2 * kSteps) return at_lane.row(grads, t, j - kSteps);
+            return at_lane.column(c < 2 * kBlocks ? grads : queries, c % kBlocks, 2 * t + c / kBlocks % 2);
         };
-        arrive_and_wait();
-        if (direct && first < last) fetch(head0, first, 0);
-        for (int head = head0; head < head1; ++head) {
-            const Scores to(p, head);
-            for (int i0 = first; i0 < last; i0 += kTileKeys, buffer ^= 1, at_lane.other(2 * L::kBytes)) {
-                if (!direct) {
-                    unsigned char* const to = lds + buffer * 2 * L::kBytes;
-                    stage<T, DP, 256>(to, p.q, head, i0, first, last, p.d, tid, entries);
-                    stage<T, DP, 256>(to + L::kBytes, p.dO, head, i0, first, last, p.d, tid, entries);
-                    if (tid < 2 * kTileKeys) {
-                        const float* const from = p.rowsums + (wave ? 0 : all) + (int64_t)head * p.mask.n + i0;
-                        of_rows[buffer][wave][lane] = i0 + lane < last ? from[lane] : 0.f;
-                    }
-                }
-                arrive_and_wait();
-                if (direct) {
-                    if (i0 + kTileKeys < last)
-                        fetch(head, i0 + kTileKeys, buffer ^ 1);
-                    else if (head + 1 < head1)
-                        fetch(head + 1, first, buffer ^ 1);
-                }
-                if (i0 >= high || i0 + kTileKeys <= low) continue;
-                const bool edge = i0 < all_low || i0 + kTileKeys > all_high;
+        s16x8 ahead[kAhead];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    f32x16 x{}, y{};
+        for (int i = 0; i < kAhead; ++i) ahead[i] = operand(i);
 #pragma unroll
-                    for (int c = 0; c < kSteps; ++c) {
-                        x = T::mfma(at_lane.row(lds, t, c), k[c], x);
-                        y = T::mfma(at_lane.row(lds + L::kBytes, t, c), v[c], y);
-                    }
-                    const float away = (float)(i0 + see.at - key + 4 * half + 32 * t);
+        for (int t = 0; t < 2; ++t) {
+            f32x16 x{}, y{}, steep{};
+            f32x4 lse[4], rowsum[4];
+            s16x8 weights[2], slopes[2];
+            float by = to.factor;
+            auto hidden = [&](int e) {
+                return (unsigned)(i0 + 4 * half + 32 * t + 8 * (e >> 2) + (e & 3) - see.lo) >= (unsigned)(see.hi - see.lo);
+            };
 #pragma unroll
-                    for (int a = 0; a < 4; ++a) {
-                        const f32x4 lse = *reinterpret_cast<const f32x4*>(&of_rows[buffer][0][32 * t + 8 * a + 4 * half]);
-                        const f32x4 rowsum = *reinterpret_cast<const f32x4*>(&of_rows[buffer][1][32 * t + 8 * a + 4 * half]);
+            for (int j = 0; j < kAll; ++j) {
+                const int i = t * kAll + j;
+                const s16x8 a = ahead[i % kAhead];
+                if (j == kSteps) {
+                    if (to.capped) {
+                        by = to.from_cap;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float steep = 1.f;
-                            const int i = 8 * a + e;
-                            const float s = to.score(x[4 * a + e], away + (float)i, steep);
-                            float weight = __builtin_amdgcn_exp2f(s - lse[e]);
-                            float slope = weight * (y[4 * a + e] - rowsum[e]) * steep;
-                            if (edge && (unsigned)(i0 + 4 * half + 32 * t + i - see.lo) >= (unsigned)(see.hi - see.lo))
-                                weight = slope = 0.f;
-                            x[4 * a + e] = weight;
-                            y[4 * a + e] = slope;
+                        for (int e = 0; e < 16; ++e) {
+                            x[e] = to.tanh_of(x[e]);
+                            steep[e] = __builtin_fmaf(-x[e], x[e], 1.f);
                         }
                     }
+                    if (to.sloped) {
+                        const float away = (float)(i0 + see.at - key + 4 * half + 32 * t);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const s16x8 weights = rounded_operand<T>(x, c), slopes = rounded_operand<T>(y, c);
-#pragma unroll
-                        for (int b = 0; b < kBlocks; ++b) {
-                            dv[b] = T::mfma(at_lane.column(lds + L::kBytes, b, 2 * t + c), weights, dv[b]);
-                            dk[b] = T::mfma(at_lane.column(lds, b, 2 * t + c), slopes, dk[b]);
-                        }
+                        for (int e = 0; e < 16; ++e)
+                            x[e] = __builtin_fmaf(-to.slope, fabsf(away + (float)(8 * (e >> 2) + (e & 3))), by * x[e]);
+                        by = 1.f;
                     }
                 }
+                if (j == 2 * kSteps) {
+                    if (edge) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = hidden(e) ? 0.f : x[e];
+                    }
+                    if (to.capped) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) steep[e] *= x[e];
+                    } else {
+                        steep = x;
+                    }
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) weights[c] = rounded_operand<T>(x, c);
+                }
+                if (j == 2 * kSteps + 2 * kBlocks) {
+                    if (edge) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) y[e] = hidden(e) ? 0.f : y[e];
+                    }
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) slopes[c] = rounded_operand<T>(y, c);
+                }
+                const int c = j - 2 * kSteps;
+                if (j < kSteps)
+                    x = T::mfma(a, k[j], x);
+                else if (j < 2 * kSteps)
+                    y = T::mfma(a, v[j - kSteps], y);
+                else if (c < 2 * kBlocks)
+                    dv[c % kBlocks] = T::mfma(a, weights[c / kBlocks], dv[c % kBlocks]);
+                else
+                    dk[c % kBlocks] = T::mfma(a, slopes[c / kBlocks - 2], dk[c % kBlocks]);
+                if (i + kAhead < 2 * kAll) ahead[i % kAhead] = operand(i + kAhead);
+                if (j < 4) {
+                    lse[j] = *reinterpret_cast<const f32x4*>(&of_rows[buffer][0][32 * t + 8 * j + 4 * half]);
+                    rowsum[j] = *reinterpret_cast<const f32x4*>(&of_rows[buffer][1][32 * t + 8 * j + 4 * half]);
+                }
+                if (j >= kSteps && j < 2 * kSteps) {
+#pragma unroll
+                    for (int e = (j - kSteps) * kEach; e < (j - kSteps + 1) * kEach && e < 16; ++e)
+                        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], by, -lse[e >> 2][e & 3]));
+                }
+                if (c >= 0 && c < 2 * kBlocks) {
+                    constexpr int kPer = (16 + 2 * kBlocks - 1) / (2 * kBlocks);
+#pragma unroll
+                    for (int e = c * kPer; e < (c + 1) * kPer && e < 16; ++e) y[e] = (y[e] - rowsum[e >> 2][e & 3]) * steep[e];
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (entries != kAsTheyAre) break;
+    };
+    auto all_finite = [&]() {
         float zero = 0.f;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(dk[b][e], 0.f, __builtin_fmaf(dv[b][e], 0.f, zero));
-        if (!__syncthreads_or(zero != 0.f)) break;
+        return !__syncthreads_or(zero != 0.f);
+    };
+    // row sums and log-sums of a tile's rows
+    auto sums_of = [&](int which, int head, int i0) { return p.rowsums + (which ? 0 : all) + (int64_t)head * p.mask.n + i0; };
+    int entries = kAsTheyAre;
+    bool done = false;
+    if (p.q.wide && p.dO.wide) {
+        int buffer = 0;
+        auto bring = [&](int head, int i0, int to) {
+            const Direct<DP, 256> from_q(p.q, head, p.d, tid), from_g(p.dO, head, p.d, tid);
+            from_q.fetch(queries + to * L::kBytes, i0, first, last, tid);
+            from_g.fetch(grads + to * L::kBytes, i0, first, last, tid);
+            if (wave < 2) fetch_words(of_rows[to][wave], sums_of(wave, head, i0), lane, last - i0);
+        };
+        begin();
+        if (first < last) bring(head0, first, 0);
+        for (int head = head0; head < head1; ++head) {
+            const Scores to(p, head);
+            for (int i0 = first; i0 < last; i0 += kTileKeys, buffer ^= 1, at_lane.other(L::kBytes)) {
+                arrive_and_wait();
+                if (i0 + kTileKeys < last)
+                    bring(head, i0 + kTileKeys, buffer ^ 1);
+                else if (head + 1 < head1)
+                    bring(head + 1, first, buffer ^ 1);
+                tile_of(to, i0, buffer);
+            }
+        }
+        done = all_finite();
+        at_lane = Lane<DP>(lane);
+        entries = kFinite;
+    }
+    // As by rows: entries of Q and dO that are not finite as zeros in a second walk.  Their rows have a log-sum or a
+    // row sum, and with it P, that is NaN.
+    for (; !done; ++entries) {
+        begin();
+        for (int head = head0; head < head1; ++head) {
+            const Scores to(p, head);
+            for (int i0 = first; i0 < last; i0 += kTileKeys) {
+                arrive_and_wait();
+                stage<T, DP, 256>(queries, p.q, head, i0, first, last, p.d, tid, entries);
+                stage<T, DP, 256>(grads, p.dO, head, i0, first, last, p.d, tid, entries);
+                if (wave < 2) of_rows[0][wave][lane] = i0 + lane < last ? sums_of(wave, head, i0)[lane] : 0.f;
+                arrive_and_wait();
+                tile_of(to, i0, 0);
+            }
+        }
+        done = entries == kFinite || all_finite();
     }
     if (!see.inside) return;
     if (p.splits > 1) {
@@ -340,9 +452,9 @@ __global__ __launch_bounds__(256) void attn_grad_join_kernel(Problem p) {
 
 template <typename T, int DP>
 hipError_t launch_kernels(const Problem& p, hipStream_t stream) {
-    const int64_t row_tiles = (p.mask.n + kTileRows - 1) / kTileRows, key_tiles = (p.mask.m + kTileRows - 1) / kTileRows;
+    const int64_t row_tiles = ((int64_t)p.mask.n * (p.hq / p.hkv) + kTileRows - 1) / kTileRows, key_tiles = (p.mask.m + kTileRows - 1) / kTileRows;
     const dim3 block(256);
-    if (row_tiles) attn_grad_rows_kernel<T, DP><<<dim3((unsigned)(row_tiles * p.hq)), block, 0, stream>>>(p);
+    if (row_tiles) attn_grad_rows_kernel<T, DP><<<dim3((unsigned)(row_tiles * p.hkv)), block, 0, stream>>>(p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !key_tiles) return e;
     attn_grad_keys_kernel<T, DP><<<dim3((unsigned)(key_tiles * p.hkv * p.splits)), block, 0, stream>>>(p);
