@@ -167,16 +167,16 @@ __device__ __forceinline__ Span rows_of_key(const Mask& k, int j) {
 
 // ---- tiles in LDS -----------------------------------------------------------------------------
 
-// 64 rows of DP entries (d rounded up; zeros behind d), row-major, a row 128 or 256 bytes.  Two readers: a
+// ROWS rows of DP entries (d rounded up; zeros behind d), row-major, a row 128 or 256 bytes.  Two readers: a
 // lane reads 16 bytes of row l % 32 (32 rows apart by whole rows: all in the same banks), and 16 lanes read
 // 32 bytes of each of 4 consecutive rows.  The 16-byte pieces of a row are therefore permuted by an exclusive-or
 // with bits of the row's number, (r1 r0 r2) below and r3 above: any eight rows in a run have different pieces, and
 // any four different pairs of pieces.
-template <int DP>
+template <int DP, int ROWS = kTileKeys>
 struct Tile {
     static constexpr int kPieces = DP <= 64 ? 8 : 16;  // of 16 bytes, in a row
     static constexpr int kRowBytes = 16 * kPieces;
-    static constexpr int kBytes = kTileKeys * kRowBytes;
+    static constexpr int kBytes = ROWS * kRowBytes;
     static __device__ __forceinline__ int turn(int row) {
         const int t = ((row & 3) << 1) | ((row >> 2) & 1);
         return kPieces == 16 ? t | (row & 8) : t;
@@ -215,14 +215,14 @@ __device__ __forceinline__ unsigned chosen(unsigned w, int entries) {
     return r;
 }
 
-// Rows first .. first + 63 of one head into LDS; those outside lo .. hi - 1 become zeros.
-template <typename T, int DP, int THREADS>
+// Rows first .. first + ROWS - 1 of one head into LDS; those outside lo .. hi - 1 become zeros.
+template <typename T, int DP, int THREADS, int ROWS = kTileKeys>
 __device__ __forceinline__ void stage(unsigned char* lds, const Rows& t, int head, int first, int lo, int hi, int d, int tid,
                                       int entries) {
     typedef Tile<DP> L;
     const unsigned short* base = t.data + head * t.hs;
 #pragma unroll 1  // (registers)
-    for (int it = 0; it < kTileKeys * L::kPieces / THREADS; ++it) {
+    for (int it = 0; it < ROWS * L::kPieces / THREADS; ++it) {
         const int at = it * THREADS + tid, r = at / L::kPieces, piece = (at % L::kPieces) ^ L::turn(r);
         const int row = first + r;
         u32x4 v = {0, 0, 0, 0};
@@ -237,11 +237,11 @@ __device__ __forceinline__ void stage(unsigned char* lds, const Rows& t, int hea
 // The same without registers in between (t.wide only): 16 bytes a lane, counted by vmcnt; the caller waits with
 // arrive_and_wait.  A lane whose piece lies outside rows or entries reads beyond the descriptor's end, which gives zeros.
 // A thread's piece is the same in every round (THREADS / kPieces is a multiple of the rows that the turn goes by).
-template <int DP, int THREADS>
+template <int DP, int THREADS, int ROWS = kTileKeys>
 struct Direct {
     typedef Tile<DP> L;
-    static constexpr int kRows = THREADS / L::kPieces, kRounds = kTileKeys / kRows;
-    static_assert(kRows % L::kPieces == 0, "");
+    static constexpr int kRows = THREADS / L::kPieces, kRounds = ROWS / kRows;
+    static_assert(kRows % L::kPieces == 0 && ROWS % kRows == 0, "");
     uint64_t base;
     unsigned offset;  // of this thread's piece; behind d: beyond the end
     int stride;       // of a row, bytes
@@ -270,7 +270,7 @@ struct Direct {
         }
     }
 };
-// Up to 64 words of one wave likewise; zeros from `count` on.
+// A word for each lane that calls likewise; zeros from `count` on.
 __device__ __forceinline__ void fetch_words(const float* lds, const float* from, int lane, int count) {
     const uint64_t base = reinterpret_cast<uint64_t>(from);
     i32x4 words;

@@ -8,51 +8,41 @@ namespace attn {
 
 namespace {
 
-// 16 products x = <Q, K> and y = <dO, V> of a tile to P and P (y - rowsum) (1 - tanh^2).  What differs between
-// calls (a cap, slopes) is asked once for the 16 and not for each; `lse` and `rowsum` give number e's log-sum, in powers
-// of two, and row sum, `far` how far its row stands from its key.
+// 16 products x = <Q, K>, less lse / scale, and y = <dO, V>, less the row sum, to P and P y (1 - tanh^2).  Both come with what
+// is taken off as their products' first summand; with a cap x comes without.  Scores are in units of the product: a cap, slopes and
+// the log-sum are divided by the scale.  `lse` gives number e's log-sum and `far` how far its row stands from its key.
 struct Scores {
     float factor, to_cap, from_cap, slope;
     bool capped, sloped;
-    __device__ __forceinline__ Scores(const Problem& p, int head) {
+    __device__ __forceinline__ Scores(const Problem& p, int head, bool any) {
         capped = p.cap > 0.f;
         sloped = p.slopes;
-        slope = sloped ? p.slopes[head] * kLog2e : 0.f;
+        slope = sloped && any ? p.slopes[head] / p.scale : 0.f;
         factor = p.scale * kLog2e;
-        to_cap = capped ? 2.f * kLog2e * p.scale / p.cap : 0.f;
-        from_cap = p.cap * kLog2e;
+        to_cap = capped ? 2.f * factor / p.cap : 0.f;
+        from_cap = p.cap / p.scale;
     }
-    __device__ __forceinline__ float tanh_of(float u) const {
-        return __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * u)), 1.f);
-    }
-    template <typename Lse, typename Sum, typename Far>
-    __device__ __forceinline__ void weights(f32x16& x, f32x16& y, Lse lse, Sum rowsum, Far far) const {
-        float by = factor;
+    template <typename Lse, typename Far>
+    __device__ __forceinline__ void weights(f32x16& x, f32x16& y, Lse lse, Far far) const {
         if (capped) {
-            by = from_cap;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                x[e] = tanh_of(x[e]);
-                y[e] = (y[e] - rowsum(e)) * __builtin_fmaf(-x[e], x[e], 1.f);
+                const float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * (x[e] + lse(e)))), 1.f);
+                y[e] *= __builtin_fmaf(-t, t, 1.f);
+                x[e] = __builtin_fmaf(from_cap, t, -lse(e));
             }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] -= rowsum(e);
         }
         if (sloped) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(-slope, fabsf(far(e)), by * x[e]);
-            by = 1.f;
+            for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(-slope, fabsf(far(e)), x[e]);
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], by, -lse(e)));
+            x[e] = __builtin_amdgcn_exp2f(x[e] * factor);
             y[e] *= x[e];
         }
     }
 };
-
-__device__ __forceinline__ float in_twos(float lse) { return lse == -kInf ? kInf : lse * kLog2e; }  // no keys: P = 0
 
 template <typename T, int DP>
 __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
@@ -101,12 +91,12 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         }
     }
     rowsum = sum_of_halves(rowsum);
-    const float lse = see.inside ? in_twos(p.lse[at]) : kInf;
+    const float log_sum = see.inside ? p.lse[at] : 0.f, lse = log_sum == -kInf ? kInf : log_sum / p.scale;  // no keys: P = 0
     if (see.inside && half == 0) {  // for the walk by keys, whose entries of Q and dO may stand in as zeros
-        p.rowsums[at] = rowsum;
-        p.rowsums[(int64_t)p.hq * p.mask.n + at] = fabsf(rowsum) < kInf ? lse : __builtin_nanf("");
+        p.rowsums[at] = fabsf(rowsum) < kInf ? -lse : __builtin_nanf("");
+        p.rowsums[(int64_t)p.hq * p.mask.n + at] = -rowsum;
     }
-    const Scores to(p, head);
+    const Scores to(p, head, see.inside);
 
     f32x16 sum[kBlocks];
     Lane<DP> at_lane(lane);
@@ -121,15 +111,18 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         const bool edge = j0 < all_low || j0 + kTileKeys > all_high;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            f32x16 x{}, y{};
+            f32x16 x, y;
+            float x_less = -lse, y_less = -rowsum;
+            asm("" : "+v"(x_less), "+v"(y_less));  // (or 32 registers hold them sixteen times all along)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = x_less, y[e] = y_less;
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) {
                 x = T::mfma(at_lane.row(keys, t, k), q[k], x);
                 y = T::mfma(at_lane.row(values, t, k), g[k], y);
             }
             const float away = (float)(see.at - j0 - 4 * half - 32 * t);
-            to.weights(x, y, [&](int) { return lse; }, [&](int) { return rowsum; },
-                       [&](int e) { return away - (float)(8 * (e >> 2) + (e & 3)); });
+            to.weights(x, y, [&](int) { return lse; }, [&](int e) { return away - (float)(8 * (e >> 2) + (e & 3)); });
             if (edge) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
@@ -200,12 +193,17 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         }
 }
 
+// By keys a step takes 32 rows, and V, the second operand of only one product, stays in LDS: so two workgroups share a
+// compute unit, one's exponentials beside the other's products (with V in registers and 64 rows a step: one, and 444 us in
+// place of XXX at 4096 rows and keys, 32 heads on 8, d = 128).
+constexpr int kStepRows = 32;
+
 template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
-    typedef Tile<DP> L;
+__global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
+    typedef Tile<DP, kStepRows> L;
     constexpr int kBlocks = DP / 32, kSteps = DP / 16;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * L::kBytes];
-    __shared__ __attribute__((aligned(16))) float of_rows[2][2][kTileKeys];  // log-sums, row sums
+    __shared__ __attribute__((aligned(16))) unsigned char lds[4 * L::kBytes + 2 * Tile<DP>::kBytes];
+    __shared__ __attribute__((aligned(16))) float of_rows[2][2][kStepRows];  // see Problem::rowsums
     __shared__ int ends[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int tiles = (p.mask.m + kTileRows - 1) / kTileRows, group = p.hq / p.hkv;
@@ -227,122 +225,64 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
     int first = ends[0], last = ends[1];
     if (first >= last) first = last = 0;
 
-    s16x8 k[kSteps], v[kSteps];
+    unsigned char* const queries = lds;
+    unsigned char* const grads = lds + 2 * L::kBytes;
+    unsigned char* const values = lds + 4 * L::kBytes;  // rows of 128 keys
+    unsigned char* const own_values = values + wave * 32 * L::kRowBytes;
+    for (int x = 0; x < 2; ++x)
+        stage<T, DP, 256>(values + x * Tile<DP>::kBytes, p.v, kv, tile * kTileRows + x * kTileKeys, 0, p.mask.m, p.d, tid, kAsTheyAre);
+    s16x8 k[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-        u32x4 a = {0, 0, 0, 0}, b = a;
-        const int column = 16 * s + 8 * half;
-        if (see.inside) {
-            a = entries8(p.k.data + key * p.k.ld + kv * p.k.hs, column, p.d, p.k.wide);
-            b = entries8(p.v.data + key * p.v.ld + kv * p.v.hs, column, p.d, p.v.wide);
-        }
+        u32x4 a = {0, 0, 0, 0};
+        if (see.inside) a = entries8(p.k.data + key * p.k.ld + kv * p.k.hs, 16 * s + 8 * half, p.d, p.k.wide);
         k[s] = __builtin_bit_cast(s16x8, a);
-        v[s] = __builtin_bit_cast(s16x8, b);
     }
 
     f32x16 dk[kBlocks], dv[kBlocks];
     Lane<DP> at_lane(lane);
-    unsigned char* const queries = lds;
-    unsigned char* const grads = lds + 2 * L::kBytes;
-    const int64_t all = (int64_t)p.hq * p.mask.n;
     const int head0 = kv * group + group * part / p.splits, head1 = kv * group + group * (part + 1) / p.splits;
     auto begin = [&]() {
         for (int b = 0; b < kBlocks; ++b) dk[b] = dv[b] = f32x16{};
     };
-    // One tile of rows that lies in LDS, 32 rows at a time: 4 products of kSteps instructions each, in the order written
-    // here.  A wave has its SIMD to itself (the accumulators alone are half of what two could have), so what would wait has to
-    // be begun early: every operand is read kAhead instructions before its own, the exponentials stand among the
-    // products of dO and V, and the rest among the sums for dV.
+    // 32 rows that lie in LDS.
     auto tile_of = [&](const Scores& to, int i0, int buffer) {
-        if (i0 >= high || i0 + kTileKeys <= low) return;
-        constexpr int kAhead = 4, kAll = 2 * kSteps + 4 * kBlocks, kEach = (16 + kSteps - 1) / kSteps;
-        const bool edge = i0 < all_low || i0 + kTileKeys > all_high;
-        auto operand = [&](int i) {
-            const int t = i / kAll, j = i % kAll, c = j - 2 * kSteps;
-            if (j < kSteps) return at_lane.row(queries, t, j);
-            if (j < 2 * kSteps) return at_lane.row(grads, t, j - kSteps);
-            return at_lane.column(c < 2 * kBlocks ? grads : queries, c % kBlocks, 2 * t + c / kBlocks % 2);
-        };
-        s16x8 ahead[kAhead];
+        if (i0 >= high || i0 + kStepRows <= low) return;
+        const unsigned own = at_lane.rows ^ (buffer ? L::kBytes : 0);
+        auto own_at = [&](int c) { return *reinterpret_cast<const s16x8*>(own_values + (own ^ (32 * c))); };
+        f32x16 x, y;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) ahead[i] = operand(i);
+        for (int a = 0; a < 4; ++a) {
+            const f32x4 lse = *reinterpret_cast<const f32x4*>(&of_rows[buffer][0][8 * a + 4 * half]);
+            const f32x4 rowsum = *reinterpret_cast<const f32x4*>(&of_rows[buffer][1][8 * a + 4 * half]);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x16 x{}, y{}, steep{};
-            f32x4 lse[4], rowsum[4];
-            s16x8 weights[2], slopes[2];
-            float by = to.factor;
-            auto hidden = [&](int e) {
-                return (unsigned)(i0 + 4 * half + 32 * t + 8 * (e >> 2) + (e & 3) - see.lo) >= (unsigned)(see.hi - see.lo);
-            };
+            for (int e = 0; e < 4; ++e) {
+                x[4 * a + e] = lse[e];
+                y[4 * a + e] = rowsum[e];
+            }
+        }
 #pragma unroll
-            for (int j = 0; j < kAll; ++j) {
-                const int i = t * kAll + j;
-                const s16x8 a = ahead[i % kAhead];
-                if (j == kSteps) {
-                    if (to.capped) {
-                        by = to.from_cap;
+        for (int c = 0; c < kSteps; ++c) {
+            x = T::mfma(at_lane.row(queries, 0, c), k[c], x);
+            y = T::mfma(at_lane.row(grads, 0, c), own_at(c), y);
+            if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+        }
+        const float away = (float)(i0 + see.at - key + 4 * half);
+        to.weights(x, y, [&](int e) { return -of_rows[buffer][0][8 * (e >> 2) + 4 * half + (e & 3)]; },
+                   [&](int e) { return away + (float)(8 * (e >> 2) + (e & 3)); });
+        if (i0 < all_low || i0 + kStepRows > all_high) {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            x[e] = to.tanh_of(x[e]);
-                            steep[e] = __builtin_fmaf(-x[e], x[e], 1.f);
-                        }
-                    }
-                    if (to.sloped) {
-                        const float away = (float)(i0 + see.at - key + 4 * half + 32 * t);
+            for (int e = 0; e < 16; ++e)
+                if ((unsigned)(i0 + 4 * half + 8 * (e >> 2) + (e & 3) - see.lo) >= (unsigned)(see.hi - see.lo)) x[e] = y[e] = 0.f;
+        }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            x[e] = __builtin_fmaf(-to.slope, fabsf(away + (float)(8 * (e >> 2) + (e & 3))), by * x[e]);
-                        by = 1.f;
-                    }
-                }
-                if (j == 2 * kSteps) {
-                    if (edge) {
+        for (int c = 0; c < 2; ++c) {
+            const s16x8 weights = rounded_operand<T>(x, c), slopes = rounded_operand<T>(y, c);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = hidden(e) ? 0.f : x[e];
-                    }
-                    if (to.capped) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) steep[e] *= x[e];
-                    } else {
-                        steep = x;
-                    }
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) weights[c] = rounded_operand<T>(x, c);
-                }
-                if (j == 2 * kSteps + 2 * kBlocks) {
-                    if (edge) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = hidden(e) ? 0.f : y[e];
-                    }
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) slopes[c] = rounded_operand<T>(y, c);
-                }
-                const int c = j - 2 * kSteps;
-                if (j < kSteps)
-                    x = T::mfma(a, k[j], x);
-                else if (j < 2 * kSteps)
-                    y = T::mfma(a, v[j - kSteps], y);
-                else if (c < 2 * kBlocks)
-                    dv[c % kBlocks] = T::mfma(a, weights[c / kBlocks], dv[c % kBlocks]);
-                else
-                    dk[c % kBlocks] = T::mfma(a, slopes[c / kBlocks - 2], dk[c % kBlocks]);
-                if (i + kAhead < 2 * kAll) ahead[i % kAhead] = operand(i + kAhead);
-                if (j < 4) {
-                    lse[j] = *reinterpret_cast<const f32x4*>(&of_rows[buffer][0][32 * t + 8 * j + 4 * half]);
-                    rowsum[j] = *reinterpret_cast<const f32x4*>(&of_rows[buffer][1][32 * t + 8 * j + 4 * half]);
-                }
-                if (j >= kSteps && j < 2 * kSteps) {
-#pragma unroll
-                    for (int e = (j - kSteps) * kEach; e < (j - kSteps + 1) * kEach && e < 16; ++e)
-                        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], by, -lse[e >> 2][e & 3]));
-                }
-                if (c >= 0 && c < 2 * kBlocks) {
-                    constexpr int kPer = (16 + 2 * kBlocks - 1) / (2 * kBlocks);
-#pragma unroll
-                    for (int e = c * kPer; e < (c + 1) * kPer && e < 16; ++e) y[e] = (y[e] - rowsum[e >> 2][e & 3]) * steep[e];
-                }
-                __builtin_amdgcn_sched_barrier(0);
+            for (int b = 0; b < kBlocks; ++b) {
+                dv[b] = T::mfma(at_lane.column(grads, b, c), weights, dv[b]);
+                dk[b] = T::mfma(at_lane.column(queries, b, c), slopes, dk[b]);
+                if (b % 2 == 1) __builtin_amdgcn_sched_barrier(0);
             }
         }
     };
@@ -354,26 +294,27 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
             for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(dk[b][e], 0.f, __builtin_fmaf(dv[b][e], 0.f, zero));
         return !__syncthreads_or(zero != 0.f);
     };
-    // row sums and log-sums of a tile's rows
-    auto sums_of = [&](int which, int head, int i0) { return p.rowsums + (which ? 0 : all) + (int64_t)head * p.mask.n + i0; };
+    auto sums_of = [&](int which, int head, int i0) {
+        return p.rowsums + ((int64_t)which * p.hq + head) * p.mask.n + i0;
+    };
     int entries = kAsTheyAre;
     bool done = false;
     if (p.q.wide && p.dO.wide) {
         int buffer = 0;
         auto bring = [&](int head, int i0, int to) {
-            const Direct<DP, 256> from_q(p.q, head, p.d, tid), from_g(p.dO, head, p.d, tid);
+            const Direct<DP, 256, kStepRows> from_q(p.q, head, p.d, tid), from_g(p.dO, head, p.d, tid);
             from_q.fetch(queries + to * L::kBytes, i0, first, last, tid);
             from_g.fetch(grads + to * L::kBytes, i0, first, last, tid);
-            if (wave < 2) fetch_words(of_rows[to][wave], sums_of(wave, head, i0), lane, last - i0);
+            if (wave < 2 && lane < kStepRows) fetch_words(of_rows[to][wave], sums_of(wave, head, i0), lane, last - i0);
         };
         begin();
         if (first < last) bring(head0, first, 0);
         for (int head = head0; head < head1; ++head) {
-            const Scores to(p, head);
-            for (int i0 = first; i0 < last; i0 += kTileKeys, buffer ^= 1, at_lane.other(L::kBytes)) {
+            const Scores to(p, head, true);
+            for (int i0 = first; i0 < last; i0 += kStepRows, buffer ^= 1, at_lane.other(L::kBytes)) {
                 arrive_and_wait();
-                if (i0 + kTileKeys < last)
-                    bring(head, i0 + kTileKeys, buffer ^ 1);
+                if (i0 + kStepRows < last)
+                    bring(head, i0 + kStepRows, buffer ^ 1);
                 else if (head + 1 < head1)
                     bring(head + 1, first, buffer ^ 1);
                 tile_of(to, i0, buffer);
@@ -388,12 +329,13 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
     for (; !done; ++entries) {
         begin();
         for (int head = head0; head < head1; ++head) {
-            const Scores to(p, head);
-            for (int i0 = first; i0 < last; i0 += kTileKeys) {
+            const Scores to(p, head, true);
+            for (int i0 = first; i0 < last; i0 += kStepRows) {
                 arrive_and_wait();
-                stage<T, DP, 256>(queries, p.q, head, i0, first, last, p.d, tid, entries);
-                stage<T, DP, 256>(grads, p.dO, head, i0, first, last, p.d, tid, entries);
-                if (wave < 2) of_rows[0][wave][lane] = i0 + lane < last ? sums_of(wave, head, i0)[lane] : 0.f;
+                stage<T, DP, 256, kStepRows>(queries, p.q, head, i0, first, last, p.d, tid, entries);
+                stage<T, DP, 256, kStepRows>(grads, p.dO, head, i0, first, last, p.d, tid, entries);
+                if (wave < 2 && lane < kStepRows)
+                    of_rows[0][wave][lane] = i0 + lane < last ? sums_of(wave, head, i0)[lane] : 0.f;
                 arrive_and_wait();
                 tile_of(to, i0, 0);
             }
@@ -401,14 +343,19 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
         done = entries == kFinite || all_finite();
     }
     if (!see.inside) return;
+    // (made again here rather than kept, in registers or beside them, from where it was first needed)
+    int tid_again = threadIdx.x;
+    asm("" : "+v"(tid_again));
+    const int half_again = (tid_again >> 5) & 1;
+    const int64_t row = tile * kTileRows + (tid_again >> 6) * 32 + (tid_again & 31);
     if (p.splits > 1) {
         const int64_t keys = (int64_t)p.mask.m * p.hkv;
-        float* const o = p.partial + (2 * part * keys + (int64_t)key * p.hkv + kv) * p.d;
+        float* const o = p.partial + (2 * part * keys + row * p.hkv + kv) * p.d;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int c = 32 * b + 8 * (e >> 2) + 4 * half + (e & 3);
+                const int c = 32 * b + 8 * (e >> 2) + 4 * half_again + (e & 3);
                 if (c >= p.d) continue;
                 o[c] = dk[b][e] * p.scale;
                 o[keys * p.d + c] = dv[b][e];
@@ -425,8 +372,8 @@ __global__ __launch_bounds__(256, 1) void attn_grad_keys_kernel(Problem p) {
                 x[e] = dk[b][4 * a + e] * p.scale;
                 y[e] = dv[b][4 * a + e];
             }
-            put4<T>(p.dk.data + key * p.dk.ld + kv * p.dk.hs, 32 * b + 8 * a + 4 * half, p.d, p.dk.wide, x);
-            put4<T>(p.dv.data + key * p.dv.ld + kv * p.dv.hs, 32 * b + 8 * a + 4 * half, p.d, p.dv.wide, y);
+            put4<T>(p.dk.data + row * p.dk.ld + kv * p.dk.hs, 32 * b + 8 * a + 4 * half_again, p.d, p.dk.wide, x);
+            put4<T>(p.dv.data + row * p.dv.ld + kv * p.dv.hs, 32 * b + 8 * a + 4 * half_again, p.d, p.dv.wide, y);
         }
 }
 

@@ -28,7 +28,7 @@ struct Problem {
     float scale, cap;
     const float* slopes;
     float* lse;      // [hq][n] or null
-    float* rowsums;  // gradient: [2][hq][n], behind the row sums the log-sums in powers of two
+    float* rowsums;  // gradient: [2][hq][n], what a row takes off its products: -log-sum / scale, -sum of dO * O
     float* partial;  // n_splits > 1
     int splits;
 };
