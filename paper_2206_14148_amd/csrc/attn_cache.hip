@@ -136,67 +136,143 @@ __device__ __forceinline__ float quotient_of(float code, float from, float to) {
     return f;
 }
 
+// A workgroup looks at `tokens` new rows for one head; where the first row of a run of rows that go to one block is among
+// them it does the run.  K and V are read twice, the second time from the caches: for the largest magnitude, then for the codes.
+// A block's codes of V lie across its rows, so they are put together in LDS and written a word of four tokens at a time; a
+// word that the run fills in part, and that is not begun anew, is written byte by byte.
+constexpr int kAppendThreads = 256;
 template <typename T>
-__device__ __forceinline__ float entry(const unsigned short* p) {
-    return T::low(*p);
-}
-
-// A wave for each new row and head; that of the first row of a run of rows that go to one block does the run.
-template <typename T>
-__global__ __launch_bounds__(256) void attn_append_kernel(AppendProblem p) {
+__global__ __launch_bounds__(kAppendThreads) void attn_append_kernel(AppendProblem p, int tokens) {
     const Cache& c = p.cache;
-    const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), first = w / c.hkv;
-    const int head = (int)(w % c.hkv);
-    if (first >= p.count) return;
-    const int64_t slots = c.blocks * c.block;
+    extern __shared__ __attribute__((aligned(16))) unsigned char turned[];  // [row][block + 4]
+    __shared__ int last_of[256];               // the last row of the run that goes to each token, -1: none
+    __shared__ unsigned covered[8];            // tokens of the block that the run writes
+    __shared__ float of_wave[2][kAppendThreads / 64];
+    __shared__ int run_end, run_fresh;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int head = blockIdx.x % c.hkv, shift = __builtin_ctz(c.block), pitch = c.block + 4;
+    const int64_t group = (int64_t)(blockIdx.x / c.hkv) * tokens, slots = c.blocks << shift;
     auto block_of = [&](int64_t t) {
         const int64_t s = p.slots[t];
-        return s >= 0 && s < slots ? s / c.block : -1;
+        return s >= 0 && s < slots ? s >> shift : -1;
     };
-    const int64_t block = block_of(first);
-    if (block < 0 || (first > 0 && block_of(first - 1) == block)) return;
-    int64_t last = first + 1;
-    while (last < p.count && block_of(last) == block) ++last;
-
-    bool fresh = false;
-    float a[2] = {0.f, 0.f};
-    for (int64_t t = first; t < last; ++t) {
-        fresh |= p.slots[t] % c.block == 0;
-        for (int col = lane; col < c.d; col += 64)
+    const int pieces = c.row / 8, per_pass = kAppendThreads / pieces, piece = tid % pieces;
+    for (int64_t first = group; first < group + tokens && first < p.count; ++first) {
+        const int64_t block = block_of(first);
+        if (block < 0 || (first > 0 && block_of(first - 1) == block)) continue;
+        __syncthreads();
+        if (tid < 8) covered[tid] = 0;
+        last_of[tid] = -1;
+        if (tid == 0) run_end = INT_MAX, run_fresh = 0;
+        __syncthreads();
+        int count = 0;  // rows of the run (slots may be given twice: it can be longer than a block)
+        for (;; count += kAppendThreads) {
+            const int64_t t = first + count + tid;
+            const bool mine = t < p.count && block_of(t) == block;
+            if (!mine) atomicMin(&run_end, count + tid);
+            __syncthreads();
+            const int found = run_end;
+            __syncthreads();
+            if (found != INT_MAX) break;
+        }
+        count = run_end;
+        float a[2] = {0.f, 0.f};
+        for (int i = tid / pieces; i < count; i += per_pass) {
+            const int64_t t = first + i;
+            const int token = (int)(p.slots[t] & (c.block - 1));
+            if (piece == 0) {
+                atomicOr(&covered[token >> 5], 1u << (token & 31));
+                atomicMax(&last_of[token], i);
+                if (token == 0) run_fresh = 1;
+            }
+#pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const Rows& r = x ? p.v : p.k;
-                const float v = fabsf(entry<T>(r.data + t * r.ld + head * r.hs + col));
-                if (v < kInf) a[x] = fmaxf(a[x], v);
-            }
-    }
-    for (int x = 0; x < 2; ++x) {
-        for (int s = 32; s; s >>= 1) a[x] = fmaxf(a[x], __shfl_xor(a[x], s));
-        float* const scale = (x ? c.v_scale : c.k_scale) + block * c.hkv + head;
-        unsigned char* const codes = (x ? c.v : c.k) + (block * c.hkv + head) * (int64_t)c.block * c.row;
-        const float before = fresh ? 0.f : *scale, after = fmaxf(before, a[x] / (c.e4m3 ? 448.f : 127.f));
-        if (fresh || after > before) {
-            for (int i = 4 * lane; i < c.block * c.row; i += 256) {
-                unsigned word = 0;
-                if (before > 0.f) {
-                    word = *reinterpret_cast<const unsigned*>(codes + i);
-                    unsigned moved = 0;
-                    for (int b = 0; b < 32; b += 8)
-                        moved |= code_of(quotient_of(value_of(word >> b & 0xffu, c.e4m3), before, after), c.e4m3) << b;
-                    word = moved;
+                const u32x4 w = entries8(r.data + t * r.ld + head * r.hs, 8 * piece, c.d, r.wide);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float low = fabsf(T::low(w[e])), high = fabsf(T::high(w[e]));
+                    if (low < kInf) a[x] = fmaxf(a[x], low);
+                    if (high < kInf) a[x] = fmaxf(a[x], high);
                 }
-                *reinterpret_cast<unsigned*>(codes + i) = word;
             }
-            if (lane == 0) *scale = after;
-            // other lanes write the new codes into those words
-            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "agent");
         }
-        for (int64_t t = first; t < last; ++t) {
-            const Rows& r = x ? p.v : p.k;
-            const int token = (int)(p.slots[t] % c.block);
-            for (int col = lane; col < c.d; col += 64) {
-                const unsigned code = code_of(quotient(entry<T>(r.data + t * r.ld + head * r.hs + col), after), c.e4m3);
-                codes[x ? col * c.block + token : token * c.row + col] = (unsigned char)code;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            for (int s = 32; s; s >>= 1) a[x] = fmaxf(a[x], __shfl_xor(a[x], s));
+            if (lane == 0) of_wave[x][wave] = a[x];
+        }
+        __syncthreads();
+        const bool fresh = run_fresh;
+        const int64_t at = block * c.hkv + head;
+#pragma unroll 1
+        for (int x = 0; x < 2; ++x) {
+            float largest = 0.f;
+            for (int w = 0; w < kAppendThreads / 64; ++w) largest = fmaxf(largest, of_wave[x][w]);
+            float* const scale = (x ? c.v_scale : c.k_scale) + at;
+            unsigned* const codes = reinterpret_cast<unsigned*>((x ? c.v : c.k) + at * (int64_t)c.block * c.row);
+            const float before = fresh ? 0.f : *scale, after = fmaxf(before, largest / (c.e4m3 ? 448.f : 127.f));
+            const bool moves = !fresh && after > before;  // codes that the block holds follow its scale
+            __syncthreads();
+            if (tid == 0) *scale = after;
+            if (moves) {
+                for (int i = tid; i < c.block * c.row / 4; i += kAppendThreads) {
+                    const unsigned word = codes[i];
+                    unsigned moved = 0;
+                    if (before > 0.f)
+                        for (int b = 0; b < 32; b += 8)
+                            moved |= code_of(quotient_of(value_of(word >> b & 0xffu, c.e4m3), before, after), c.e4m3) << b;
+                    codes[i] = moved;
+                }
+            }
+            // other waves write the new codes into those words: the stores have to be done, not only begun (a fence for
+            // the whole device would write the L2 back, 40 us)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            for (int i = tid / pieces; i < count; i += per_pass) {
+                const int64_t t = first + i;
+                const int token = (int)(p.slots[t] & (c.block - 1));
+                if (last_of[token] != i) continue;  // a slot given twice
+                const Rows& r = x ? p.v : p.k;
+                const u32x4 v = entries8(r.data + t * r.ld + head * r.hs, 8 * piece, c.d, r.wide);
+                u32x2 w = {0, 0};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = e & 1 ? T::high(v[e / 2]) : T::low(v[e / 2]);
+                    w[e / 4] |= code_of(quotient(y, after), c.e4m3) << (8 * (e % 4));
+                }
+                if (x == 0) {
+                    *reinterpret_cast<u32x2*>(codes + (token * c.row + 8 * piece) / 4) = w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) turned[(8 * piece + e) * pitch + token] = (unsigned char)(w[e / 4] >> (8 * (e % 4)));
+                }
+            }
+            __syncthreads();
+            if (x == 0) {
+                if (fresh)
+                    for (int i = tid; i < c.block * c.row / 4; i += kAppendThreads) {
+                        const int token = 4 * i / c.row;
+                        if (!(covered[token >> 5] >> (token & 31) & 1)) codes[i] = 0;
+                    }
+            } else {
+                for (int i = tid; i < c.block * c.row / 4; i += kAppendThreads) {
+                    const int token = 4 * i & (c.block - 1), line = 4 * i >> shift;
+                    const unsigned have = covered[token >> 5] >> (token & 31) & 15u;
+                    if (!have && !fresh) continue;
+                    unsigned word = 0;
+                    if (have) word = *reinterpret_cast<const unsigned*>(turned + line * pitch + token);
+                    const unsigned mask = (have & 1 ? 0xffu : 0) | (have & 2 ? 0xff00u : 0) | (have & 4 ? 0xff0000u : 0) |
+                                          (have & 8 ? 0xff000000u : 0);
+                    if (fresh || have == 15u) {
+                        codes[i] = word & mask;
+                    } else {
+                        unsigned char* const bytes = reinterpret_cast<unsigned char*>(codes + i);
+                        for (int b = 0; b < 4; ++b)
+                            if (have >> b & 1) bytes[b] = (unsigned char)(word >> (8 * b));
+                    }
+                }
             }
         }
     }
@@ -493,11 +569,15 @@ hipError_t launch_map(const MapProblem& p, hipStream_t stream) {
 }
 
 hipError_t launch_append(const AppendProblem& p, hipStream_t stream) {
-    const dim3 grid((unsigned)((p.count * p.cache.hkv + 3) / 4));
+    // A workgroup for each row and head where few rows are each likely to go to a block of their own (a step's); where
+    // there are many, most go where the row before went, and a workgroup looks at as many as the smallest block holds.
+    const int tokens = p.count * p.cache.hkv <= 4096 ? 1 : 16;
+    const dim3 grid((unsigned)((p.count + tokens - 1) / tokens * p.cache.hkv)), block(kAppendThreads);
+    const size_t lds = (size_t)p.cache.row * (p.cache.block + 4);
     if (p.f16)
-        attn_append_kernel<F16><<<grid, dim3(256), 0, stream>>>(p);
+        attn_append_kernel<F16><<<grid, block, lds, stream>>>(p, tokens);
     else
-        attn_append_kernel<Bf16><<<grid, dim3(256), 0, stream>>>(p);
+        attn_append_kernel<Bf16><<<grid, block, lds, stream>>>(p, tokens);
     return hipGetLastError();
 }
 

@@ -376,16 +376,25 @@ __device__ __forceinline__ float2 join_ranges(const float* partial, int ranges, 
     total *= f;
     x[0] = x[1] = 0.f;
     float all = 0.f;
+    // eight at a time, so that their loads are under way together
     const float* o = partial + at * d + lane;
     const bool in0 = lane < d, in1 = 64 + lane < d;
-#pragma unroll 8
-    for (int s = 0; s < used; ++s, o += rows * d) {
-        const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
-        const float a = in0 ? o[0] : 0.f, b = in1 ? o[64] : 0.f;
-        all += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(total), s));
-        // (zero times an infinity, of a range whose weights have vanished against another's: nothing)
-        x[0] = __builtin_fmaf(fs != 0.f ? a : 0.f, fs, x[0]);
-        x[1] = __builtin_fmaf(fs != 0.f ? b : 0.f, fs, x[1]);
+    for (int s0 = 0; s0 < used; s0 += 8) {
+        float a[8], b[8];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float* const from = o + (s0 + s) * rows * d;
+            a[s] = s0 + s < used && in0 ? from[0] : 0.f;
+            b[s] = s0 + s < used && in1 ? from[64] : 0.f;
+        }
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s0 + s));
+            all += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(total), s0 + s));
+            // (zero times an infinity, of a range whose weights have vanished against another's: nothing)
+            x[0] = __builtin_fmaf(fs != 0.f ? a[s] : 0.f, fs, x[0]);
+            x[1] = __builtin_fmaf(fs != 0.f ? b[s] : 0.f, fs, x[1]);
+        }
     }
     return float2{most, all};
 }
