@@ -106,28 +106,44 @@ __global__ __launch_bounds__(kMapThreads) void attn_map_kernel(MapProblem p) {
 
 // ---- new rows ---------------------------------------------------------------------------------
 
-__device__ __forceinline__ float value_of(unsigned code, int e4m3) {
-    return e4m3 ? __builtin_amdgcn_cvt_f32_fp8(code, 0) : (float)(signed char)code;
+template <bool E4M3>
+__device__ __forceinline__ float value_of(unsigned code) {
+    if constexpr (E4M3) return __builtin_amdgcn_cvt_f32_fp8(code, 0);
+    return (float)(signed char)code;
 }
 
 // The code nearest to y; y is exact or rounded to odd (its last bit says that something was cut off), so that the
 // one rounding here is that of the real number.
-__device__ __forceinline__ unsigned code_of(float y, int e4m3) {
-    if (!(fabsf(y) >= 0.f)) return 0;  // NaN
-    if (e4m3) return __builtin_amdgcn_cvt_pk_fp8_f32(fminf(fmaxf(y, -448.f), 448.f), 0.f, 0, false) & 0xffu;
-    return (unsigned)(int)__builtin_rintf(fminf(fmaxf(y, -127.f), 127.f)) & 0xffu;
+template <bool E4M3>
+__device__ __forceinline__ unsigned code_of(float y) {
+    constexpr float kMost = E4M3 ? 448.f : 127.f;
+    y = y == y ? fminf(fmaxf(y, -kMost), kMost) : 0.f;
+    if constexpr (E4M3) return __builtin_amdgcn_cvt_pk_fp8_f32(y, 0.f, 0, false) & 0xffu;
+    return (unsigned)(int)__builtin_rintf(y) & 0xffu;
 }
 
-__device__ __forceinline__ float quotient(float x, float s) {
-    if (s == 0.f) return 0.f;
-    const float y = x / s;
-    const unsigned bits = __float_as_uint(y);
-    if ((bits & 1) || !(fabsf(y) < kInf)) return y;
-    const float rest = __builtin_fmaf(-y, s, x);  // exact: its sign says on which side of y the quotient lies
-    if (rest == 0.f) return y;
-    return __uint_as_float((rest < 0.f) == (y < 0.f) ? bits | 1 : bits - 1);
-}
+// x / s rounded to odd, by s and 1 / s (a division for each would be three times the instructions).  Both are taken times
+// 2^100 where s is so small that 1 / s may be infinite; of s = 0 every quotient is 0.
+struct Divisor {
+    float s, inverse, times;
+    __device__ __forceinline__ explicit Divisor(float s_) {
+        times = s_ == 0.f ? 0.f : s_ < 0x1p-100f ? 0x1p100f : 1.f;
+        s = s_ == 0.f ? 1.f : s_ * times;
+        inverse = 1.f / s;
+    }
+    __device__ __forceinline__ float operator()(float x) const {
+        x *= times;
+        float y = x * inverse;
+        y = __builtin_fmaf(__builtin_fmaf(-y, s, x), inverse, y);
+        const unsigned bits = __float_as_uint(y);
+        const float rest = __builtin_fmaf(-y, s, x);  // exact: its sign says on which side of y the quotient lies
+        const unsigned odd = (rest < 0.f) == (y < 0.f) ? bits | 1 : bits - 1;
+        y = (bits & 1) || rest == 0.f ? y : __uint_as_float(odd);
+        return fabsf(x) < kInf ? y : x;
+    }
+};
 
+// code * from / to likewise
 __device__ __forceinline__ float quotient_of(float code, float from, float to) {
     const double y = (double)code * from / to;
     float f = (float)y;
@@ -137,65 +153,86 @@ __device__ __forceinline__ float quotient_of(float code, float from, float to) {
 }
 
 // A workgroup looks at `tokens` new rows for one head; where the first row of a run of rows that go to one block is among
-// them it does the run.  K and V are read twice, the second time from the caches: for the largest magnitude, then for the codes.
-// A block's codes of V lie across its rows, so they are put together in LDS and written a word of four tokens at a time; a
-// word that the run fills in part, and that is not begun anew, is written byte by byte.
-constexpr int kAppendThreads = 256;
-template <typename T>
+// them it does the run.  What bounds it for a step's few rows is one memory access waiting for another: slots, then rows and
+// scales, then the codes go out.  Rows are kept in registers from the search of the largest magnitude to the codes where four
+// passes of the workgroup hold them (64 rows of 128), else read again.  A block's codes of V lie across its rows, so they are
+// put together in LDS and written a word of four tokens at a time; a word that the run fills in part, and that is not begun
+// anew, is written byte by byte.
+constexpr int kAppendThreads = 256, kAppendPasses = 4;
+template <typename T, bool E4M3>
 __global__ __launch_bounds__(kAppendThreads) void attn_append_kernel(AppendProblem p, int tokens) {
     const Cache& c = p.cache;
     extern __shared__ __attribute__((aligned(16))) unsigned char turned[];  // [row][block + 4]
     __shared__ int last_of[256];               // the last row of the run that goes to each token, -1: none
+    __shared__ int token_of[kAppendThreads];   // of the run's first rows
     __shared__ unsigned covered[8];            // tokens of the block that the run writes
+    __shared__ unsigned char moved_to[2][256];  // what becomes of each code that the block holds
     __shared__ float of_wave[2][kAppendThreads / 64];
-    __shared__ int run_end, run_fresh;
+    __shared__ int run_end;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int head = blockIdx.x % c.hkv, shift = __builtin_ctz(c.block), pitch = c.block + 4;
     const int64_t group = (int64_t)(blockIdx.x / c.hkv) * tokens, slots = c.blocks << shift;
     auto block_of = [&](int64_t t) {
-        const int64_t s = p.slots[t];
+        const int64_t s = t >= 0 && t < p.count ? p.slots[t] : -1;
         return s >= 0 && s < slots ? s >> shift : -1;
     };
-    const int pieces = c.row / 8, per_pass = kAppendThreads / pieces, piece = tid % pieces;
-    for (int64_t first = group; first < group + tokens && first < p.count; ++first) {
-        const int64_t block = block_of(first);
-        if (block < 0 || (first > 0 && block_of(first - 1) == block)) continue;
+    // lane l looks at row group + l: whether a run begins there
+    const int64_t mine = lane < tokens ? block_of(group + lane) : -1, before_mine = lane < tokens ? block_of(group + lane - 1) : -1;
+    unsigned long long firsts = __ballot(mine >= 0 && mine != before_mine);
+    const int pieces = c.row / 8, per_pass = kAppendThreads / pieces, piece = tid % pieces, line = tid / pieces;
+    while (firsts) {
+        const int64_t first = group + __builtin_ctzll(firsts), block = block_of(first), at = block * c.hkv + head;
+        firsts &= firsts - 1;
         __syncthreads();
         if (tid < 8) covered[tid] = 0;
         last_of[tid] = -1;
-        if (tid == 0) run_end = INT_MAX, run_fresh = 0;
+        if (tid == 0) run_end = INT_MAX;
+        const float scales[2] = {c.k_scale[at], c.v_scale[at]};
         __syncthreads();
         int count = 0;  // rows of the run (slots may be given twice: it can be longer than a block)
         for (;; count += kAppendThreads) {
             const int64_t t = first + count + tid;
-            const bool mine = t < p.count && block_of(t) == block;
-            if (!mine) atomicMin(&run_end, count + tid);
+            if (block_of(t) != block)
+                atomicMin(&run_end, count + tid);
+            else if (count == 0)
+                token_of[tid] = (int)(p.slots[t] & (c.block - 1));
             __syncthreads();
             const int found = run_end;
             __syncthreads();
             if (found != INT_MAX) break;
         }
         count = run_end;
-        float a[2] = {0.f, 0.f};
-        for (int i = tid / pieces; i < count; i += per_pass) {
-            const int64_t t = first + i;
-            const int token = (int)(p.slots[t] & (c.block - 1));
-            if (piece == 0) {
-                atomicOr(&covered[token >> 5], 1u << (token & 31));
-                atomicMax(&last_of[token], i);
-                if (token == 0) run_fresh = 1;
-            }
+        auto token = [&](int i) { return i < kAppendThreads ? token_of[i] : (int)(p.slots[first + i] & (c.block - 1)); };
+        u32x4 rows[2][kAppendPasses];
+        auto read = [&](int i0) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const Rows& r = x ? p.v : p.k;
-                const u32x4 w = entries8(r.data + t * r.ld + head * r.hs, 8 * piece, c.d, r.wide);
+            for (int x = 0; x < 2; ++x)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float low = fabsf(T::low(w[e])), high = fabsf(T::high(w[e]));
-                    if (low < kInf) a[x] = fmaxf(a[x], low);
-                    if (high < kInf) a[x] = fmaxf(a[x], high);
+                for (int n = 0; n < kAppendPasses; ++n) {
+                    const int i = i0 + line * kAppendPasses + n;
+                    const Rows& r = x ? p.v : p.k;
+                    rows[x][n] = u32x4{0, 0, 0, 0};
+                    if (i < count) rows[x][n] = entries8(r.data + (first + i) * r.ld + head * r.hs, 8 * piece, c.d, r.wide);
                 }
+        };
+        float a[2] = {0.f, 0.f};
+        const int round = kAppendPasses * per_pass;
+        for (int i0 = 0; i0 < count; i0 += round) {
+            read(i0);
+            for (int i = i0 + tid; i < min(i0 + round, count); i += kAppendThreads) {
+                const int to = token(i);
+                atomicOr(&covered[to >> 5], 1u << (to & 31));
+                atomicMax(&last_of[to], i);
             }
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int n = 0; n < kAppendPasses; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float low = fabsf(T::low(rows[x][n][e])), high = fabsf(T::high(rows[x][n][e]));
+                        a[x] = fmaxf(a[x], fmaxf(low < kInf ? low : 0.f, high < kInf ? high : 0.f));
+                    }
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -203,26 +240,28 @@ __global__ __launch_bounds__(kAppendThreads) void attn_append_kernel(AppendProbl
             if (lane == 0) of_wave[x][wave] = a[x];
         }
         __syncthreads();
-        const bool fresh = run_fresh;
-        const int64_t at = block * c.hkv + head;
-#pragma unroll 1
+        const bool fresh = covered[0] & 1;  // token 0: begun anew
+        float after[2];
+        bool moves[2];
         for (int x = 0; x < 2; ++x) {
             float largest = 0.f;
             for (int w = 0; w < kAppendThreads / 64; ++w) largest = fmaxf(largest, of_wave[x][w]);
-            float* const scale = (x ? c.v_scale : c.k_scale) + at;
-            unsigned* const codes = reinterpret_cast<unsigned*>((x ? c.v : c.k) + at * (int64_t)c.block * c.row);
-            const float before = fresh ? 0.f : *scale, after = fmaxf(before, largest / (c.e4m3 ? 448.f : 127.f));
-            const bool moves = !fresh && after > before;  // codes that the block holds follow its scale
+            const float before = fresh ? 0.f : scales[x];
+            after[x] = fmaxf(before, largest / (E4M3 ? 448.f : 127.f));
+            if (tid == 0) (x ? c.v_scale : c.k_scale)[at] = after[x];
+            moves[x] = !fresh && after[x] > before;  // codes that the block holds follow its scale
+            if (moves[x])
+                moved_to[x][tid] = before > 0.f ? (unsigned char)code_of<E4M3>(quotient_of(value_of<E4M3>(tid), before, after[x])) : 0;
+        }
+        if (moves[0] || moves[1]) {
             __syncthreads();
-            if (tid == 0) *scale = after;
-            if (moves) {
+            for (int x = 0; x < 2; ++x) {
+                if (!moves[x]) continue;
+                unsigned* const codes = reinterpret_cast<unsigned*>((x ? c.v : c.k) + at * (int64_t)c.block * c.row);
                 for (int i = tid; i < c.block * c.row / 4; i += kAppendThreads) {
-                    const unsigned word = codes[i];
-                    unsigned moved = 0;
-                    if (before > 0.f)
-                        for (int b = 0; b < 32; b += 8)
-                            moved |= code_of(quotient_of(value_of(word >> b & 0xffu, c.e4m3), before, after), c.e4m3) << b;
-                    codes[i] = moved;
+                    const unsigned w = codes[i];
+                    codes[i] = moved_to[x][w & 255] | moved_to[x][w >> 8 & 255] << 8 | moved_to[x][w >> 16 & 255] << 16 |
+                               (unsigned)moved_to[x][w >> 24] << 24;
                 }
             }
             // other waves write the new codes into those words: the stores have to be done, not only begun (a fence for
@@ -230,49 +269,69 @@ __global__ __launch_bounds__(kAppendThreads) void attn_append_kernel(AppendProbl
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
-            for (int i = tid / pieces; i < count; i += per_pass) {
-                const int64_t t = first + i;
-                const int token = (int)(p.slots[t] & (c.block - 1));
-                if (last_of[token] != i) continue;  // a slot given twice
-                const Rows& r = x ? p.v : p.k;
-                const u32x4 v = entries8(r.data + t * r.ld + head * r.hs, 8 * piece, c.d, r.wide);
-                u32x2 w = {0, 0};
+        }
+        const Divisor by[2] = {Divisor(after[0]), Divisor(after[1])};
+        unsigned char* const k_codes = c.k + at * (int64_t)c.block * c.row;
+        unsigned* const v_codes = reinterpret_cast<unsigned*>(c.v + at * (int64_t)c.block * c.row);
+        for (int i0 = 0; i0 < count; i0 += round) {
+            if (count > round) read(i0);
+            // a thread's four rows mostly go to four tokens in a row
+            if (i0 + line * kAppendPasses >= count) continue;
+            int to[kAppendPasses];
+            u32x2 w[kAppendPasses];
+            bool together = true;
+#pragma unroll
+            for (int n = 0; n < kAppendPasses; ++n) {
+                const int i = i0 + line * kAppendPasses + n;
+                to[n] = i < count ? token(i) : -1;
+                if (to[n] >= 0 && last_of[to[n]] != i) to[n] = -1;  // a slot given twice
+                together = together && to[n] >= 0 && to[n] == to[0] + n;
+                w[n] = u32x2{0, 0};
+                if (to[n] < 0) continue;
+                u32x2 k = {0, 0};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float y = e & 1 ? T::high(v[e / 2]) : T::low(v[e / 2]);
-                    w[e / 4] |= code_of(quotient(y, after), c.e4m3) << (8 * (e % 4));
+                    const unsigned a = rows[0][n][e / 2], b = rows[1][n][e / 2];
+                    k[e / 4] |= code_of<E4M3>(by[0](e & 1 ? T::high(a) : T::low(a))) << (8 * (e % 4));
+                    w[n][e / 4] |= code_of<E4M3>(by[1](e & 1 ? T::high(b) : T::low(b))) << (8 * (e % 4));
                 }
-                if (x == 0) {
-                    *reinterpret_cast<u32x2*>(codes + (token * c.row + 8 * piece) / 4) = w;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) turned[(8 * piece + e) * pitch + token] = (unsigned char)(w[e / 4] >> (8 * (e % 4)));
-                }
+                *reinterpret_cast<u32x2*>(k_codes + to[n] * c.row + 8 * piece) = k;
             }
-            __syncthreads();
-            if (x == 0) {
-                if (fresh)
-                    for (int i = tid; i < c.block * c.row / 4; i += kAppendThreads) {
-                        const int token = 4 * i / c.row;
-                        if (!(covered[token >> 5] >> (token & 31) & 1)) codes[i] = 0;
-                    }
-            } else {
-                for (int i = tid; i < c.block * c.row / 4; i += kAppendThreads) {
-                    const int token = 4 * i & (c.block - 1), line = 4 * i >> shift;
-                    const unsigned have = covered[token >> 5] >> (token & 31) & 15u;
-                    if (!have && !fresh) continue;
-                    unsigned word = 0;
-                    if (have) word = *reinterpret_cast<const unsigned*>(turned + line * pitch + token);
-                    const unsigned mask = (have & 1 ? 0xffu : 0) | (have & 2 ? 0xff00u : 0) | (have & 4 ? 0xff0000u : 0) |
-                                          (have & 8 ? 0xff000000u : 0);
-                    if (fresh || have == 15u) {
-                        codes[i] = word & mask;
-                    } else {
-                        unsigned char* const bytes = reinterpret_cast<unsigned char*>(codes + i);
-                        for (int b = 0; b < 4; ++b)
-                            if (have >> b & 1) bytes[b] = (unsigned char)(word >> (8 * b));
-                    }
+            static_assert(kAppendPasses == 4, "");
+            if (together && to[0] % 4 == 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    unsigned v = 0;
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) v |= (w[n][e / 4] >> (8 * (e % 4)) & 0xffu) << (8 * n);
+                    *reinterpret_cast<unsigned*>(turned + (8 * piece + e) * pitch + to[0]) = v;
                 }
+            } else {
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+                    if (to[n] >= 0)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            turned[(8 * piece + e) * pitch + to[n]] = (unsigned char)(w[n][e / 4] >> (8 * (e % 4)));
+            }
+        }
+        __syncthreads();
+        for (int i = tid; i < c.block * c.row / 4; i += kAppendThreads) {
+            if (fresh) {
+                const int to = 4 * i / c.row;
+                if (!(covered[to >> 5] >> (to & 31) & 1)) reinterpret_cast<unsigned*>(k_codes)[i] = 0;
+            }
+            const int to = 4 * i & (c.block - 1), column = 4 * i >> shift;
+            const unsigned have = covered[to >> 5] >> (to & 31) & 15u;
+            if (!have && !fresh) continue;
+            const unsigned word = have ? *reinterpret_cast<const unsigned*>(turned + column * pitch + to) : 0;
+            const unsigned mask = (have & 1 ? 0xffu : 0) | (have & 2 ? 0xff00u : 0) | (have & 4 ? 0xff0000u : 0) | (have & 8 ? 0xff000000u : 0);
+            if (fresh || have == 15u) {
+                v_codes[i] = word & mask;
+            } else {
+                unsigned char* const bytes = reinterpret_cast<unsigned char*>(v_codes + i);
+                for (int b = 0; b < 4; ++b)
+                    if (have >> b & 1) bytes[b] = (unsigned char)(word >> (8 * b));
             }
         }
     }
@@ -574,10 +633,9 @@ hipError_t launch_append(const AppendProblem& p, hipStream_t stream) {
     const int tokens = p.count * p.cache.hkv <= 4096 ? 1 : 16;
     const dim3 grid((unsigned)((p.count + tokens - 1) / tokens * p.cache.hkv)), block(kAppendThreads);
     const size_t lds = (size_t)p.cache.row * (p.cache.block + 4);
-    if (p.f16)
-        attn_append_kernel<F16><<<grid, block, lds, stream>>>(p, tokens);
-    else
-        attn_append_kernel<Bf16><<<grid, block, lds, stream>>>(p, tokens);
+    auto kernel = p.f16 ? (p.cache.e4m3 ? attn_append_kernel<F16, true> : attn_append_kernel<F16, false>)
+                        : (p.cache.e4m3 ? attn_append_kernel<Bf16, true> : attn_append_kernel<Bf16, false>);
+    kernel<<<grid, block, lds, stream>>>(p, tokens);
     return hipGetLastError();
 }
 
