@@ -1,9 +1,15 @@
 """ctypes binding of the attention entry points (include/attn.h): argument marshalling only."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 from dataclasses import dataclass
+
+try:  # plans need no tensors
+    import torch
+except ImportError:
+    torch = None
 
 from . import binding as _b
 from .binding import KNN_ERR_HIP, KNN_ERR_INVALID_ARG, KNN_OK, KnnError, knn_status_string
@@ -74,13 +80,13 @@ class AttnPlan:
     min_limit_bytes: int
 
 
-_ready = False
+_lib = None
 
 
 def _load():
-    global _ready
-    lib = _b.load()
-    if not _ready:
+    global _lib
+    if _lib is None:
+        lib = _b.load()
         i64, i32, u64, vp, ptr = ctypes.c_int64, ctypes.c_int32, ctypes.c_uint64, ctypes.c_void_p, ctypes.POINTER
         shape, rows = [i64, i64, i32, i32, i32], ptr(RowsStruct)
         lib.attn_plan.argtypes = lib.attn_grad_plan.argtypes = shape + [u64, ptr(AttnPlanStruct)]
@@ -96,8 +102,22 @@ def _load():
                                          vp, u64, vp, u64, rows, vp]
         for name in ATTN_SYMBOLS:
             getattr(lib, name).restype = ctypes.c_int
-        _ready = True
-    return lib
+        _lib = lib
+    return _lib
+
+
+_same_device = contextlib.nullcontext()
+
+
+def _on(device):
+    """The device as the current one; nothing to do where it is."""
+    return _same_device if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _stream(device) -> int:
+    # (the object that torch makes around it would cost more than all checks of a call)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
 
 
 def _raise(st: int, plan=None):
@@ -107,20 +127,23 @@ def _raise(st: int, plan=None):
     raise KnnError(st, detail, int(plan.min_limit_bytes) if plan is not None else 0)
 
 
-def _plan(fn, n, m, hq, hkv, d, mem_limit_bytes) -> AttnPlan:
-    ps = AttnPlanStruct()
-    st = int(fn(n, m, hq, hkv, d, mem_limit_bytes, ctypes.byref(ps)))
+def _planned(fn, ps, *shape):
+    st = int(fn(*shape, ctypes.byref(ps)))
     if st != KNN_OK:
         _raise(st, ps)
-    return AttnPlan(*(getattr(ps, f[0]) for f in AttnPlanStruct._fields_ if f[0] != "reserved"))
+    return ps
+
+
+def _as(cls, ps):
+    return cls(*(getattr(ps, name) for name in cls.__dataclass_fields__))
 
 
 def attn_plan(n: int, m: int, hq: int, hkv: int, d: int, mem_limit_bytes: int) -> AttnPlan:
-    return _plan(_load().attn_plan, n, m, hq, hkv, d, mem_limit_bytes)
+    return _as(AttnPlan, _planned(_load().attn_plan, AttnPlanStruct(), n, m, hq, hkv, d, mem_limit_bytes))
 
 
 def attn_grad_plan(n: int, m: int, hq: int, hkv: int, d: int, mem_limit_bytes: int) -> AttnPlan:
-    return _plan(_load().attn_grad_plan, n, m, hq, hkv, d, mem_limit_bytes)
+    return _as(AttnPlan, _planned(_load().attn_grad_plan, AttnPlanStruct(), n, m, hq, hkv, d, mem_limit_bytes))
 
 
 def _refuse(text):
@@ -149,8 +172,6 @@ def _words(name, t, device, count, dtype):
 
 
 def _dtype(Q):
-    import torch
-
     if not Q.is_cuda:
         _refuse("Q must be a device tensor (no CPU path exists)")
     if Q.dtype not in (torch.bfloat16, torch.float16):
@@ -169,8 +190,6 @@ def _shape(Q, K, V):
 
 
 def _options(Q, scale, causal, cap, slopes, starts, k_starts, prefix):
-    import torch
-
     dtype = _dtype(Q)
     if k_starts is None:
         k_starts = starts
@@ -188,14 +207,16 @@ def _options(Q, scale, causal, cap, slopes, starts, k_starts, prefix):
 
 
 def _workspace(workspace, nbytes, device):
-    import torch
-
+    """(the tensor, which the call keeps alive, its address and size)"""
     if workspace is None:
-        return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+        if not nbytes:
+            return None, None, 0
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return workspace, workspace.data_ptr(), nbytes
     if not workspace.is_cuda or workspace.device != device or workspace.dtype != torch.uint8 or \
             not workspace.is_contiguous():
         _refuse(f"workspace must be contiguous uint8 on {device}")
-    return workspace
+    return workspace, workspace.data_ptr(), workspace.numel()
 
 
 def attn_apply(Q, K, V, mem_limit_bytes: int, scale=None, causal: bool = False, cap: float = 0.0, slopes=None,
@@ -210,13 +231,11 @@ def attn_apply(Q, K, V, mem_limit_bytes: int, scale=None, causal: bool = False, 
     documents keep what `out` (O, lse) holds there.  The workspace (uint8, attn_plan's bytes) is
     allocated here unless given.  Work is enqueued on torch's current stream; no synchronisation is done.
     """
-    import torch
-
     options = _options(Q, scale, causal, cap, slopes, starts, k_starts, prefix)
     n, m, hq, hkv, d = _shape(Q, K, V)
-    plan = attn_plan(n, m, hq, hkv, d, mem_limit_bytes)
-    with torch.cuda.device(Q.device):
-        workspace = _workspace(workspace, plan.workspace_bytes, Q.device)
+    plan = _planned(_load().attn_plan, AttnPlanStruct(), n, m, hq, hkv, d, mem_limit_bytes)
+    with _on(Q.device):
+        workspace, ws, ws_bytes = _workspace(workspace, plan.workspace_bytes, Q.device)
         if out is None:
             O = torch.empty((n, hq, d), dtype=Q.dtype, device=Q.device)
             lse = torch.empty((hq, n), dtype=torch.float32, device=Q.device)
@@ -225,16 +244,14 @@ def attn_apply(Q, K, V, mem_limit_bytes: int, scale=None, causal: bool = False, 
             _check_rows("O", O, Q, (n, hq, d))
             _check_lse(lse, hq, n, Q.device)
         st = int(_load().attn_apply(_rows(Q), _rows(K), _rows(V), n, m, hq, hkv, d, options, mem_limit_bytes,
-                                    workspace.data_ptr(), workspace.numel(), _rows(O), lse.data_ptr(),
-                                    torch.cuda.current_stream(Q.device).cuda_stream))
+                                    ws, ws_bytes, _rows(O), lse.data_ptr(),
+                                    _stream(Q.device)))
     if st != KNN_OK:
         _raise(st)
     return O, lse
 
 
 def _check_lse(lse, hq, n, device):
-    import torch
-
     if not lse.is_cuda or lse.device != device or lse.dtype != torch.float32 or tuple(lse.shape) != (hq, n) or \
             not lse.is_contiguous():
         _refuse(f"lse must be contiguous float32 [{hq}, {n}] on {device}")
@@ -248,16 +265,14 @@ def attn_grad(Q, K, V, O, lse, dO, mem_limit_bytes: int, scale=None, causal: boo
     options.  Heads that share a K and V add up.  The workspace (uint8, attn_grad_plan's bytes) is allocated here
     unless given; `out` takes the three gradients.  The same inputs give the same bits.
     """
-    import torch
-
     options = _options(Q, scale, causal, cap, slopes, starts, k_starts, prefix)
     n, m, hq, hkv, d = _shape(Q, K, V)
     _check_rows("O", O, Q, (n, hq, d))
     _check_rows("dO", dO, Q, (n, hq, d))
     _check_lse(lse, hq, n, Q.device)
-    plan = attn_grad_plan(n, m, hq, hkv, d, mem_limit_bytes)
-    with torch.cuda.device(Q.device):
-        workspace = _workspace(workspace, plan.workspace_bytes, Q.device)
+    plan = _planned(_load().attn_grad_plan, AttnPlanStruct(), n, m, hq, hkv, d, mem_limit_bytes)
+    with _on(Q.device):
+        workspace, ws, ws_bytes = _workspace(workspace, plan.workspace_bytes, Q.device)
         if out is None:
             dQ = torch.empty((n, hq, d), dtype=Q.dtype, device=Q.device)
             dK, dV = (torch.empty((m, hkv, d), dtype=Q.dtype, device=Q.device) for _ in range(2))
@@ -267,8 +282,8 @@ def attn_grad(Q, K, V, O, lse, dO, mem_limit_bytes: int, scale=None, causal: boo
             _check_rows("dK", dK, Q, (m, hkv, d))
             _check_rows("dV", dV, Q, (m, hkv, d))
         st = int(_load().attn_grad(_rows(Q), _rows(K), _rows(V), _rows(O), lse.data_ptr(), _rows(dO), n, m, hq, hkv, d,
-                                   options, mem_limit_bytes, workspace.data_ptr(), workspace.numel(), _rows(dQ),
-                                   _rows(dK), _rows(dV), torch.cuda.current_stream(Q.device).cuda_stream))
+                                   options, mem_limit_bytes, ws, ws_bytes, _rows(dQ),
+                                   _rows(dK), _rows(dV), _stream(Q.device)))
     if st != KNN_OK:
         _raise(st)
     return dQ, dK, dV
@@ -295,8 +310,6 @@ class AttnCache:
     @staticmethod
     def empty(blocks: int, hkv: int, d: int, block: int, code: str = "int8", device="cuda") -> "AttnCache":
         """A cache of nothing yet; code "int8" or "e4m3"."""
-        import torch
-
         dtype = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[code]
         row = attn_cache_row(d)
         k = torch.zeros((blocks, hkv, block, row), dtype=torch.uint8, device=device).view(dtype)
@@ -310,35 +323,32 @@ class AttnCache:
         return _b.knn_chunk_rows(limit_bytes, hkv * (2 * block * attn_cache_row(d) + 8))
 
     def _struct(self):
-        import torch
-
-        k, v = self.k, self.v
-        if k.dim() != 4 or v.dim() != 4 or not k.is_cuda:
+        k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
+        if k.dim() != 4 or not k.is_cuda:
             _refuse("k and v must be 4-D device tensors")
-        blocks, hkv, block, row = k.shape
-        if row != attn_cache_row(self.d) or tuple(v.shape) != (blocks, hkv, row, block):
-            _refuse(f"k must be [blocks, hkv, block, {attn_cache_row(self.d)}] and v the same with the last two exchanged")
-        if k.dtype not in (torch.int8, torch.float8_e4m3fn) or v.dtype != k.dtype or v.device != k.device or \
-                not k.is_contiguous() or not v.is_contiguous():
+        blocks, hkv, block, row = shape = k.shape
+        if row != (64 if self.d <= 64 else 128) or not 1 <= self.d <= ATTN_MAX_D or v.shape != (blocks, hkv, row, block):
+            _refuse("k must be [blocks, hkv, block, attn_cache_row(d)] and v the same with the last two exchanged")
+        code = _codes().get(k.dtype)
+        device = k.device
+        if code is None or v.dtype != k.dtype or v.device != device or not k.is_contiguous() or not v.is_contiguous():
             _refuse("k and v must be contiguous, both int8 or both float8_e4m3fn, on one device")
-        for t in (self.k_scale, self.v_scale):
-            if t.dtype != torch.float32 or t.device != k.device or tuple(t.shape) != (blocks, hkv) or not t.is_contiguous():
+        for t in (ks, vs):
+            if t.dtype != torch.float32 or t.device != device or t.shape != shape[:2] or not t.is_contiguous():
                 _refuse("k_scale and v_scale must be contiguous float32 [blocks, hkv] on the device of k")
-        return CacheStruct(k.data_ptr(), v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), blocks, hkv,
-                           self.d, block, ATTN_INT8 if k.dtype == torch.int8 else ATTN_E4M3)
+        return CacheStruct(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), blocks, hkv, self.d, block, code)
+
+
+def _codes():
+    return {torch.int8: ATTN_INT8, torch.float8_e4m3fn: ATTN_E4M3}
 
 
 def attn_cache_plan(batch: int, nq: int, hq: int, hkv: int, d: int, longest: int, mem_limit_bytes: int) -> AttnCachePlan:
-    ps = AttnCachePlanStruct()
-    st = int(_load().attn_cache_plan(batch, nq, hq, hkv, d, longest, mem_limit_bytes, ctypes.byref(ps)))
-    if st != KNN_OK:
-        _raise(st, ps)
-    return AttnCachePlan(*(getattr(ps, f[0]) for f in AttnCachePlanStruct._fields_))
+    return _as(AttnCachePlan, _planned(_load().attn_cache_plan, AttnCachePlanStruct(), batch, nq, hq, hkv, d, longest,
+                                       mem_limit_bytes))
 
 
 def _check_table(table, batch, device):
-    import torch
-
     if not table.is_cuda or table.device != device or table.dtype != torch.int32 or table.dim() != 2 or \
             table.shape[0] != batch or not table.is_contiguous():
         _refuse(f"table must be contiguous int32 [{batch}, width] on {device}")
@@ -353,15 +363,13 @@ def attn_cache_map(lengths, news, table, free, block: int, n_slots: int, out=Non
     starts[i + 1] - 1 and go to slots; -1 behind the last and where there is no block.  `used` entries of `free` are
     needed; more than it has: too few.  `out` takes (starts, slots, used).
     """
-    import torch
-
     if not lengths.is_cuda:
         _refuse("lengths must be a device tensor (no CPU path exists)")
     device, batch = lengths.device, lengths.numel()
     _check_table(table, batch, device)
     pointers = (_words("lengths", lengths, device, batch, torch.int32), _words("news", news, device, batch, torch.int32))
     free_ptr = _words("free", free, device, None, torch.int32)
-    with torch.cuda.device(device):
+    with _on(device):
         if out is None:
             starts = torch.empty((batch + 1,), dtype=torch.int32, device=device)
             slots = torch.empty((n_slots,), dtype=torch.int64, device=device)
@@ -373,7 +381,7 @@ def attn_cache_map(lengths, news, table, free, block: int, n_slots: int, out=Non
             _words("used", used, device, 1, torch.int32)
         st = int(_load().attn_cache_map(*pointers, batch, table.data_ptr(), table.shape[1], block, free_ptr, free.numel(),
                                         starts.data_ptr(), slots.data_ptr(), n_slots, used.data_ptr(),
-                                        torch.cuda.current_stream(device).cuda_stream))
+                                        _stream(device)))
     if st != KNN_OK:
         _raise(st)
     return table, starts, slots, used
@@ -385,8 +393,6 @@ def attn_cache_append(cache: AttnCache, K, V, slots) -> None:
     The slots of one block must stand together; -1 is passed over.  A block's scale grows with its largest magnitude,
     codes that it holds already follow; a block that gets its token 0 is begun anew.
     """
-    import torch
-
     c = cache._struct()
     if not K.is_cuda or K.device != cache.k.device:
         _refuse("K and V must be on the cache's device")
@@ -397,9 +403,9 @@ def attn_cache_append(cache: AttnCache, K, V, slots) -> None:
     _check_rows("K", K, K, (count, c.hkv, c.d))
     _check_rows("V", V, K, (count, c.hkv, c.d))
     at = _words("slots", slots, K.device, count, torch.int64)
-    with torch.cuda.device(K.device):
+    with _on(K.device):
         st = int(_load().attn_cache_append(c, dtype, _rows(K), _rows(V), count, at,
-                                           torch.cuda.current_stream(K.device).cuda_stream))
+                                           _stream(K.device)))
     if st != KNN_OK:
         _raise(st)
 
@@ -412,8 +418,6 @@ def attn_cache_apply(Q, cache: AttnCache, table, lengths, mem_limit_bytes: int, 
     own among them: row t sees tokens up to lengths - nq + t.  scale, cap and slopes as in attn_apply.  The workspace
     (uint8, attn_cache_plan's bytes for longest = width * block) is allocated here unless given.
     """
-    import torch
-
     c = cache._struct()
     if not Q.is_cuda or Q.device != cache.k.device or Q.dim() != 4:
         _refuse("Q must be [batch, nq, hq, d] on the cache's device")
@@ -424,9 +428,10 @@ def attn_cache_apply(Q, cache: AttnCache, table, lengths, mem_limit_bytes: int, 
     _check_table(table, batch, Q.device)
     at = _words("lengths", lengths, Q.device, batch, torch.int32)
     tilt = _words("slopes", slopes, Q.device, hq, torch.float32)
-    plan = attn_cache_plan(batch, nq, hq, c.hkv, d, table.shape[1] * c.block, mem_limit_bytes)
-    with torch.cuda.device(Q.device):
-        workspace = _workspace(workspace, plan.workspace_bytes, Q.device)
+    plan = _planned(_load().attn_cache_plan, AttnCachePlanStruct(), batch, nq, hq, c.hkv, d, table.shape[1] * c.block,
+                    mem_limit_bytes)
+    with _on(Q.device):
+        workspace, ws, ws_bytes = _workspace(workspace, plan.workspace_bytes, Q.device)
         O = torch.empty((batch, nq, hq, d), dtype=Q.dtype, device=Q.device) if out is None else out
         if not O.is_cuda or O.device != Q.device or O.dtype != Q.dtype or O.shape != Q.shape or (d > 1 and O.stride(3) != 1):
             _refuse(f"out must be {tuple(Q.shape)} in {Q.dtype} on {Q.device} with unit stride along its last dimension")
@@ -437,8 +442,8 @@ def attn_cache_apply(Q, cache: AttnCache, table, lengths, mem_limit_bytes: int, 
             flat.append(RowsStruct(t.data_ptr() if t.numel() else None, t.stride(1) if nq > 1 else t.stride(0), t.stride(2)))
         st = int(_load().attn_cache_apply(c, dtype, flat[0], batch, nq, hq, table.data_ptr(), table.shape[1], at,
                                           1.0 / math.sqrt(d) if scale is None else float(scale), float(cap), tilt,
-                                          mem_limit_bytes, workspace.data_ptr(), workspace.numel(), flat[1],
-                                          torch.cuda.current_stream(Q.device).cuda_stream))
+                                          mem_limit_bytes, ws, ws_bytes, flat[1],
+                                          _stream(Q.device)))
     if st != KNN_OK:
         _raise(st)
     return O

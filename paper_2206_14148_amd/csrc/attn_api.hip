@@ -36,8 +36,8 @@ knn_status check_shape(int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t d,
     std::memset(out, 0, sizeof(*out));
     if (n < 0 || m < 0 || hkv < 1 || hq < hkv || hq % hkv != 0 || d < 1) return KNN_ERR_INVALID_ARG;
     if (d > ATTN_MAX_D || n > kMostRows || m > kMostRows || hq > 65535) return KNN_ERR_UNSUPPORTED;
-    // one workgroup for each tile and head, at most 64 ranges each
-    if ((n / attn::kTileRows + 1) * hq > (1 << 23) || (m / attn::kTileRows + 1) * hq > (1 << 23)) return KNN_ERR_UNSUPPORTED;
+    // rows times heads in 32 bits; one workgroup for each tile and head, at most 64 ranges each
+    if ((n / attn::kTileRows + 1) * hq >= (1 << 24) || (m / attn::kTileRows + 1) * hq >= (1 << 24)) return KNN_ERR_UNSUPPORTED;
     out->n = n;
     out->m = m;
     out->hq = hq;
@@ -227,9 +227,10 @@ bool cache_of(const attn_cache_t* c, attn::Cache* out) {
 }
 
 // Tokens that one workgroup walks: so many ranges that the longest request alone, and the batch at about half
-// of its length, occupy the GPU, but no fewer tokens than its four waves take at once.
+// of its length, occupy the GPU.  Below 512 tokens a range the join, a launch of its own, costs more than the walk.
 constexpr int64_t kWantCache = 4 * knn::kNumCU;
-constexpr int64_t kLeastTokens = 256;
+constexpr int64_t kLeastTokens = 512;
+constexpr int64_t kStepTokens = 256;  // that its four waves take at once
 
 }  // namespace
 
@@ -293,14 +294,14 @@ extern "C" knn_status attn_cache_plan(int64_t batch, int32_t nq, int32_t hq, int
     while (sets > 0 && sets * ranges < kWantCache && ranges < attn::kMaxSplits && longest / (2 * ranges) >= kLeastTokens &&
            bytes(2 * ranges) <= mem_limit_bytes)
         ranges *= 2;
-    const int64_t tokens = ((longest + ranges - 1) / ranges + kLeastTokens - 1) / kLeastTokens * kLeastTokens;
+    const int64_t tokens = ((longest + ranges - 1) / ranges + kStepTokens - 1) / kStepTokens * kStepTokens;
     out->batch = batch;
     out->longest = longest;
     out->nq = nq;
     out->hq = hq;
     out->hkv = hkv;
     out->d = d;
-    out->range_tokens = (int32_t)(tokens ? tokens : kLeastTokens);
+    out->range_tokens = (int32_t)(tokens ? tokens : kStepTokens);
     out->n_ranges = tokens ? (int32_t)((longest + tokens - 1) / tokens) : 1;
     out->workspace_bytes = bytes(out->n_ranges);
     return KNN_OK;

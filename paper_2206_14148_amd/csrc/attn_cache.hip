@@ -350,8 +350,12 @@ __device__ __forceinline__ f16x8 halves_of(u32x2 w) {
             const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[e], 1.f, true);
             r[4 * e] = a[0], r[4 * e + 1] = a[1], r[4 * e + 2] = b[0], r[4 * e + 3] = b[1];
         } else {
-#pragma unroll
-            for (int b = 0; b < 4; ++b) r[4 * e + b] = (_Float16)(short)(signed char)(w[e] >> (8 * b));
+            // c + 128 below the byte 0x64 is 1024 + 128 + c in f16, exactly
+            const unsigned u = w[e] ^ 0x80808080u;
+            const f16x2 less = {(_Float16)-1152.f, (_Float16)-1152.f};
+            const f16x2 a = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x07010700u)) + less;
+            const f16x2 b = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x07030702u)) + less;
+            r[4 * e] = a[0], r[4 * e + 1] = a[1], r[4 * e + 2] = b[0], r[4 * e + 3] = b[1];
         }
     }
     return r;
@@ -507,10 +511,14 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheProblem p) {
                 for (int e = 0; e < 4; ++e) most = fmaxf(most, x[t][e]);
             most = fmaxf(most, __shfl_xor(most, 16));
             most = fmaxf(most, __shfl_xor(most, 32));
-            const float now = fmaxf(top[s], most), base = now == -kInf ? 0.f : now;
-            const float shrink = __builtin_amdgcn_exp2f(top[s] - base);
-            top[s] = now;
-            total[s] *= shrink;
+            if (__any(most > top[s])) {
+                const float now = fmaxf(top[s], most), shrink = top[s] == now ? 1.f : __builtin_amdgcn_exp2f(top[s] - now);
+                top[s] = now;
+                total[s] *= shrink;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) sum[s][t] *= shrink;
+            }
+            const float base = top[s] == -kInf ? 0.f : top[s];
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -529,7 +537,7 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheProblem p) {
                 y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<E4M3>(u32x2{vc[t][0], vc[t][1]}), weights[0], y, 0, 0, 0);
                 y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<E4M3>(u32x2{vc[t][2], vc[t][3]}), weights[1], y, 0, 0, 0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[s][t][e] = __builtin_fmaf(y[e], vmost, sum[s][t][e] * shrink);
+                for (int e = 0; e < 4; ++e) sum[s][t][e] = __builtin_fmaf(y[e], vmost, sum[s][t][e]);
             }
         }
     }
