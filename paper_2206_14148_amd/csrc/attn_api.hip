@@ -228,7 +228,7 @@ bool cache_of(const attn_cache_t* c, attn::Cache* out) {
 
 // Tokens that one workgroup walks: so many ranges that the longest request alone, and the batch at about half
 // of its length, occupy the GPU.  Below 512 tokens a range the join, a launch of its own, costs more than the walk.
-constexpr int64_t kWantCache = 4 * knn::kNumCU;
+constexpr int64_t kWantCache = 8 * knn::kNumCU;
 constexpr int64_t kLeastTokens = 512;
 constexpr int64_t kStepTokens = 256;  // that its four waves take at once
 

@@ -395,9 +395,10 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheProblem p) {
     const Cache& c = p.cache;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
     const int group = p.hq / c.hkv, rows = p.nq * group, row_sets = (rows + 16 * SETS - 1) / (16 * SETS);
-    const int w = work_of(blockIdx.x, gridDim.x);
-    const int range = w % p.ranges, set = w / p.ranges % row_sets, head = w / p.ranges / row_sets % c.hkv;
-    const int b = w / p.ranges / row_sets / c.hkv;
+    // Heads go round first: the eight XCDs take workgroups in turn, so each gets its share of every request (in runs of
+    // requests the longest ones made some XCDs work half as long again as others).
+    const int w = blockIdx.x, head = w % c.hkv, set = w / c.hkv % row_sets, b = w / c.hkv / row_sets % p.batch;
+    const int range = w / c.hkv / row_sets / p.batch;
     const int length = min(max(p.lengths[b], 0), p.width * c.block);
     const int begin = range * p.range_tokens, end = min(length, begin + p.range_tokens);
     // (of an empty request the first range writes the rows)
