@@ -23,9 +23,10 @@ constexpr int64_t kMostRows = (int64_t)1 << 30;
 // registers are those of two; with a causal mask the first keys' are twice as long as the mean, so that four rounds of
 // shorter ones end sooner than one of long ones, although the parts have to be written and read.
 constexpr int64_t kWantRows = 2 * knn::kNumCU, kWantKeys = 4 * knn::kNumCU;
-// A range of keys is worth a workgroup of its own from this many on: its sums are written and read once more, 4 d bytes a
-// row each way, against 4 d bytes a key read.
-constexpr int64_t kLeastRange = 256;
+// A range of keys is worth a workgroup of its own from this many on (two tiles): 3 rows of 16 heads against 50021 keys took 34 us
+// in ranges of 782 keys and XXX in ranges of 196.  Below kLeastSplit keys the join, a launch of its own, costs more than
+// half the walk.  One part of the gradient by keys has kLeastSteps steps at least.
+constexpr int64_t kLeastRange = 128, kLeastSplit = 512, kLeastSteps = 16;
 
 uint64_t part_bytes(int64_t n, int32_t hq, int32_t d, int64_t splits) {
     return splits > 1 ? knn::align_up((uint64_t)splits * n * hq * (d + 2) * 4) : 0;
@@ -105,7 +106,7 @@ extern "C" knn_status attn_plan(int64_t n, int64_t m, int32_t hq, int32_t hkv, i
     if (st != KNN_OK) return st;
     const int64_t tiles = (n * (hq / hkv) + attn::kTileRows - 1) / attn::kTileRows * hkv;
     int64_t s = 1;
-    while (tiles > 0 && tiles * s < kWantRows && 2 * s <= attn::kMaxSplits && m / (2 * s) >= kLeastRange &&
+    while (m >= kLeastSplit && tiles > 0 && tiles * s < kWantRows && 2 * s <= attn::kMaxSplits && m / (2 * s) >= kLeastRange &&
            part_bytes(n, hq, d, 2 * s) <= mem_limit_bytes)
         s *= 2;
     out->n_splits = (int32_t)s;
@@ -121,9 +122,10 @@ extern "C" knn_status attn_grad_plan(int64_t n, int64_t m, int32_t hq, int32_t h
     out->min_limit_bytes = sums;
     if (mem_limit_bytes < sums) return KNN_ERR_MEM_LIMIT_TOO_SMALL;
     const int64_t tiles = (m + attn::kTileRows - 1) / attn::kTileRows * hkv;
+    const int64_t steps = (n + attn::kStepRows - 1) / attn::kStepRows * (hq / hkv);
     auto bytes = [&](int64_t s) { return s > 1 ? knn::align_up((uint64_t)s * 2 * m * hkv * d * 4) : 0; };
     int64_t s = 1;
-    while (tiles > 0 && tiles * s < kWantKeys && 2 * s <= hq / hkv && 2 * s <= attn::kMaxSplits &&
+    while (tiles > 0 && tiles * s < kWantKeys && 2 * s <= attn::kMaxSplits && steps / (2 * s) >= kLeastSteps &&
            sums + bytes(2 * s) <= mem_limit_bytes)
         s *= 2;
     out->n_splits = (int32_t)s;
@@ -230,6 +232,7 @@ bool cache_of(const attn_cache_t* c, attn::Cache* out) {
 // of its length, occupy the GPU.  Below 512 tokens a range the join, a launch of its own, costs more than the walk.
 constexpr int64_t kWantCache = 8 * knn::kNumCU;
 constexpr int64_t kLeastTokens = 512;
+constexpr int64_t kMostRanges = 64;
 constexpr int64_t kStepTokens = 256;  // that its four waves take at once
 
 }  // namespace
@@ -291,7 +294,7 @@ extern "C" knn_status attn_cache_plan(int64_t batch, int32_t nq, int32_t hq, int
         return ranges > 1 ? knn::align_up((uint64_t)ranges * batch * nq * hq * (d + 2) * 4) : 0;
     };
     int64_t ranges = 1;
-    while (sets > 0 && sets * ranges < kWantCache && ranges < attn::kMaxSplits && longest / (2 * ranges) >= kLeastTokens &&
+    while (sets > 0 && sets * ranges < kWantCache && ranges < kMostRanges && longest / (2 * ranges) >= kLeastTokens &&
            bytes(2 * ranges) <= mem_limit_bytes)
         ranges *= 2;
     const int64_t tokens = ((longest + ranges - 1) / ranges + kStepTokens - 1) / kStepTokens * kStepTokens;

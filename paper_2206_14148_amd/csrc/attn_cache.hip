@@ -592,11 +592,10 @@ __global__ __launch_bounds__(256) void attn_cache_join_kernel(CacheProblem p) {
     const int row = (int)(at % rows), head = (int)(at / rows % c.hkv), b = (int)(at / rows / c.hkv);
     const int length = min(max(p.lengths[b], 0), p.width * c.block);
     const int ranges = max(1, (length + p.range_tokens - 1) / p.range_tokens);
-    float x[2];
-    const float total = join_ranges(p.partial, p.ranges, ranges, all, at, c.d, lane, x).y;
+    const Joined r = join_ranges<1>(p.partial, p.ranges, ranges, all, at, c.d, lane, 0);
     unsigned short* const o = p.o.data + ((int64_t)b * p.nq + row / group) * p.o.ld + (head * group + row % group) * p.o.hs;
     for (int e = 0; e < 2; ++e)
-        if (64 * e + lane < c.d) o[64 * e + lane] = (unsigned short)T::pack(total == 0.f ? 0.f : x[e] / total, 0.f);
+        if (64 * e + lane < c.d) o[64 * e + lane] = (unsigned short)T::pack(r.total == 0.f ? 0.f : r.x[e] / r.total, 0.f);
 }
 
 template <typename T, bool E4M3, int ROW>

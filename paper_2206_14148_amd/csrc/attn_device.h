@@ -357,29 +357,34 @@ __device__ __forceinline__ void put4(unsigned short* p, int c, int d, int wide, 
 }
 
 // The sums of one row over ranges of its keys: partial [ranges][rows][d], behind it [ranges][rows] maximum (in powers of two)
-// and total.  x: entries lane and 64 + lane; returns maximum (0 if there is none) and total.  One wave, at most 64 ranges
-// of which the first `used` hold something.
-__device__ __forceinline__ float2 join_ranges(const float* partial, int ranges, int used, int64_t rows, int64_t at, int d, int lane,
-                                              float* x) {
+// and total.  A wave for up to 64 ranges, lane s looking after one; WAVES waves for a row, whose sums meet in LDS.
+struct Joined {
+    float top, total;  // top: 0 if there is no key
+    float x[2];        // entries lane and 64 + lane
+};
+template <int WAVES>
+__device__ __forceinline__ Joined join_ranges(const float* partial, int ranges, int used, int64_t rows, int64_t at, int d, int lane,
+                                              int wave) {
     const float* const ends = partial + ranges * rows * d;
+    const int first = WAVES == 1 ? 0 : 64 * wave;
+    used -= first;
     float top = -kInf, total = 0.f;
     if (lane < used) {
-        const float2 e = *reinterpret_cast<const float2*>(ends + 2 * (lane * rows + at));
+        const float2 e = *reinterpret_cast<const float2*>(ends + 2 * ((first + lane) * rows + at));
         top = e.x;
         total = e.y;
     }
     float most = top;
 #pragma unroll
     for (int s = 32; s; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
-    if (most == -kInf) most = 0.f;
-    const float f = __builtin_amdgcn_exp2f(top - most);
+    const float base = most == -kInf ? 0.f : most;
+    const float f = __builtin_amdgcn_exp2f(top - base);
     total *= f;
-    x[0] = x[1] = 0.f;
-    float all = 0.f;
+    Joined r{base, 0.f, {0.f, 0.f}};
     // eight at a time, so that their loads are under way together
-    const float* o = partial + at * d + lane;
+    const float* o = partial + (first * rows + at) * d + lane;
     const bool in0 = lane < d, in1 = 64 + lane < d;
-    for (int s0 = 0; s0 < used; s0 += 8) {
+    for (int s0 = 0; s0 < min(used, 64); s0 += 8) {
         float a[8], b[8];
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
@@ -390,13 +395,33 @@ __device__ __forceinline__ float2 join_ranges(const float* partial, int ranges, 
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
             const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s0 + s));
-            all += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(total), s0 + s));
+            r.total += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(total), s0 + s));
             // (zero times an infinity, of a range whose weights have vanished against another's: nothing)
-            x[0] = __builtin_fmaf(fs != 0.f ? a[s] : 0.f, fs, x[0]);
-            x[1] = __builtin_fmaf(fs != 0.f ? b[s] : 0.f, fs, x[1]);
+            r.x[0] = __builtin_fmaf(fs != 0.f ? a[s] : 0.f, fs, r.x[0]);
+            r.x[1] = __builtin_fmaf(fs != 0.f ? b[s] : 0.f, fs, r.x[1]);
         }
     }
-    return float2{most, all};
+    if constexpr (WAVES > 1) {
+        __shared__ float of_wave[WAVES][130];
+        of_wave[wave][lane] = r.x[0];
+        of_wave[wave][64 + lane] = r.x[1];
+        if (lane == 0) {
+            of_wave[wave][128] = most;
+            of_wave[wave][129] = r.total;
+        }
+        __syncthreads();
+        most = of_wave[0][128];
+        for (int w = 1; w < WAVES; ++w) most = fmaxf(most, of_wave[w][128]);
+        r.top = most == -kInf ? 0.f : most;
+        r.total = r.x[0] = r.x[1] = 0.f;
+        for (int w = 0; w < WAVES; ++w) {
+            const float fw = __builtin_amdgcn_exp2f(of_wave[w][128] - r.top);
+            r.total = __builtin_fmaf(of_wave[w][129], fw, r.total);
+            r.x[0] = __builtin_fmaf(fw != 0.f ? of_wave[w][lane] : 0.f, fw, r.x[0]);
+            r.x[1] = __builtin_fmaf(fw != 0.f ? of_wave[w][64 + lane] : 0.f, fw, r.x[1]);
+        }
+    }
+    return r;
 }
 
 }  // namespace

@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     constexpr int kBlocks = DP / 32, kSteps = DP / 16;
     __shared__ __attribute__((aligned(16))) unsigned char lds[4 * L::kBytes];
     __shared__ int ends[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     // The heads that share a K and V stand side by side: "rows" of the tile are rows and, within a row, its heads.
     const int group = p.hq / p.hkv, tiles = (int)(((int64_t)p.mask.n * group + kTileRows - 1) / kTileRows);
     const int w = work_of(blockIdx.x, gridDim.x);
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
         atomicMax(&ends[1], high);
     }
     __syncthreads();
-    int first = ends[0], last = ends[1];
+    int first = __builtin_amdgcn_readfirstlane(ends[0]), last = __builtin_amdgcn_readfirstlane(ends[1]);
     if (first >= last) first = last = 0;
     const int steps = (last - first + kTileKeys - 1) / kTileKeys;
     const int s0 = (int)((int64_t)steps * split / p.splits), s1 = (int)((int64_t)steps * (split + 1) / p.splits);
@@ -247,24 +247,23 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     }
 }
 
-// The ranges' sums of one row, in ascending order: a wave for each row and head.  Lane s looks after range s.
-static_assert(kMaxSplits <= 64, "");
-template <typename T>
+// The ranges' sums of one row, in ascending order: WAVES waves for each row and head.
+static_assert(kMaxSplits <= 4 * 64, "");
+template <typename T, int WAVES>
 __global__ __launch_bounds__(256) void attn_join_kernel(Problem p) {
-    const int lane = threadIdx.x & 63;
-    const int64_t rows = (int64_t)p.hq * p.mask.n, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t rows = (int64_t)p.hq * p.mask.n, at = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
     if (at >= rows) return;
     const int head = (int)(at / p.mask.n), row = (int)(at % p.mask.n);
     if (!keys_of_row(p.mask, row).inside) return;
-    float x[2];
-    const float2 ends = join_ranges(p.partial, p.splits, p.splits, rows, at, p.d, lane, x);
-    const float top = ends.x, total = ends.y;
-    const float inverse = total == 0.f ? 0.f : 1.f / total;
+    const Joined r = join_ranges<WAVES>(p.partial, p.splits, p.splits, rows, at, p.d, lane, wave);
+    if (WAVES > 1 && wave > 0) return;
+    const float inverse = r.total == 0.f ? 0.f : 1.f / r.total;
     for (int e = 0; e < 2; ++e)
         if (64 * e + lane < p.d)
             p.o.data[row * p.o.ld + head * p.o.hs + 64 * e + lane] =
-                (unsigned short)T::pack(total == 0.f ? 0.f : x[e] * inverse, 0.f);
-    if (p.lse && lane == 0) p.lse[at] = total == 0.f ? -kInf : (top + __builtin_amdgcn_logf(total)) * kLn2;
+                (unsigned short)T::pack(r.total == 0.f ? 0.f : r.x[e] * inverse, 0.f);
+    if (p.lse && lane == 0) p.lse[at] = r.total == 0.f ? -kInf : (r.top + __builtin_amdgcn_logf(r.total)) * kLn2;
 }
 
 template <typename T>
@@ -280,7 +279,10 @@ hipError_t launch(const Problem& p, hipStream_t stream) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t rows = (int64_t)p.hq * p.mask.n;
-    attn_join_kernel<T><<<dim3((unsigned)((rows + 3) / 4)), block, 0, stream>>>(p);
+    if (p.splits <= 64)
+        attn_join_kernel<T, 1><<<dim3((unsigned)((rows + 3) / 4)), block, 0, stream>>>(p);
+    else
+        attn_join_kernel<T, 4><<<dim3((unsigned)rows), block, 0, stream>>>(p);
     return hipGetLastError();
 }
 

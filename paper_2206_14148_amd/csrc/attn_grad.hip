@@ -12,15 +12,19 @@ namespace {
 // is taken off as their products' first summand; with a cap x comes without.  Scores are in units of the product: a cap, slopes and
 // the log-sum are divided by the scale.  `lse` gives number e's log-sum and `far` how far its row stands from its key.
 struct Scores {
-    float factor, to_cap, from_cap, slope;
+    float factor, to_cap, from_cap, slope, per_scale;
     bool capped, sloped;
-    __device__ __forceinline__ Scores(const Problem& p, int head, bool any) {
+    __device__ __forceinline__ explicit Scores(const Problem& p) {
         capped = p.cap > 0.f;
         sloped = p.slopes;
-        slope = sloped && any ? p.slopes[head] / p.scale : 0.f;
+        slope = 0.f;
+        per_scale = 1.f / p.scale;
         factor = p.scale * kLog2e;
         to_cap = capped ? 2.f * factor / p.cap : 0.f;
         from_cap = p.cap / p.scale;
+    }
+    __device__ __forceinline__ void of_head(const Problem& p, int head) {
+        if (sloped) slope = p.slopes[head] * per_scale;
     }
     template <typename Lse, typename Far>
     __device__ __forceinline__ void weights(f32x16& x, f32x16& y, Lse lse, Far far) const {
@@ -50,7 +54,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     constexpr int kBlocks = DP / 32, kSteps = DP / 16;
     __shared__ __attribute__((aligned(16))) unsigned char lds[4 * L::kBytes];
     __shared__ int ends[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     // (rows and, within a row, the heads that share a K and V, as in the forward pass)
     const int group = p.hq / p.hkv, tiles = (int)(((int64_t)p.mask.n * group + kTileRows - 1) / kTileRows);
     const int w = work_of(blockIdx.x, gridDim.x);
@@ -67,7 +71,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         atomicMax(&ends[1], high);
     }
     __syncthreads();
-    int first = ends[0], last = ends[1];
+    int first = __builtin_amdgcn_readfirstlane(ends[0]), last = __builtin_amdgcn_readfirstlane(ends[1]);
     if (first >= last) first = last = 0;
 
     const int64_t at = (int64_t)head * p.mask.n + row;
@@ -96,7 +100,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         p.rowsums[at] = fabsf(rowsum) < kInf ? -lse : __builtin_nanf("");
         p.rowsums[(int64_t)p.hq * p.mask.n + at] = -rowsum;
     }
-    const Scores to(p, head, see.inside);
+    Scores to(p);
+    if (see.inside) to.of_head(p, head);
 
     f32x16 sum[kBlocks];
     Lane<DP> at_lane(lane);
@@ -196,8 +201,6 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
 // By keys a step takes 32 rows, and V, the second operand of only one product, stays in LDS: so two workgroups share a
 // compute unit, one's exponentials beside the other's products (with V in registers and 64 rows a step: one, and 444 us in
 // place of XXX at 4096 rows and keys, 32 heads on 8, d = 128).
-constexpr int kStepRows = 32;
-
 template <typename T, int DP>
 __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     typedef Tile<DP, kStepRows> L;
@@ -205,7 +208,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     __shared__ __attribute__((aligned(16))) unsigned char lds[4 * L::kBytes + 2 * Tile<DP>::kBytes];
     __shared__ __attribute__((aligned(16))) float of_rows[2][2][kStepRows];  // see Problem::rowsums
     __shared__ int ends[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const int tiles = (p.mask.m + kTileRows - 1) / kTileRows, group = p.hq / p.hkv;
     const int w = work_of(blockIdx.x, gridDim.x);
     // the first keys first: with a causal mask most rows see them
@@ -222,7 +225,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
         atomicMax(&ends[1], high);
     }
     __syncthreads();
-    int first = ends[0], last = ends[1];
+    int first = __builtin_amdgcn_readfirstlane(ends[0]), last = __builtin_amdgcn_readfirstlane(ends[1]);
     if (first >= last) first = last = 0;
 
     unsigned char* const queries = lds;
@@ -241,12 +244,26 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
 
     f32x16 dk[kBlocks], dv[kBlocks];
     Lane<DP> at_lane(lane);
-    const int head0 = kv * group + group * part / p.splits, head1 = kv * group + group * (part + 1) / p.splits;
+    // This part's steps, of those through all rows of all heads that read K and V: from row0 of head0 to before row1 of the
+    // last head.
+    const int through = (last - first + kStepRows - 1) / kStepRows;
+    const int step0 = (int)((int64_t)through * group * part / p.splits), step1 = (int)((int64_t)through * group * (part + 1) / p.splits);
+    int head0 = 0, head1 = 0, row0 = 0, row1 = 0;
+    if (step0 < step1) {
+        head0 = kv * group + step0 / through;
+        head1 = kv * group + (step1 - 1) / through + 1;
+        row0 = first + step0 % through * kStepRows;
+        row1 = first + ((step1 - 1) % through + 1) * kStepRows;
+    }
     auto begin = [&]() {
         for (int b = 0; b < kBlocks; ++b) dk[b] = dv[b] = f32x16{};
     };
+    // of a lane's first row of a tile: how far past the key it stands, and past the first row that sees the key
+    const int from_key = see.at - key + 4 * half, from_first = 4 * half - see.lo;
+    const unsigned seen = see.hi - see.lo;
     // 32 rows that lie in LDS.
-    auto tile_of = [&](const Scores& to, int i0, int buffer) {
+    Scores to(p);
+    auto tile_of = [&](int i0, int buffer) {
         if (i0 >= high || i0 + kStepRows <= low) return;
         const unsigned own = at_lane.rows ^ (buffer ? L::kBytes : 0);
         auto own_at = [&](int c) { return *reinterpret_cast<const s16x8*>(own_values + (own ^ (32 * c))); };
@@ -267,13 +284,13 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
             y = T::mfma(at_lane.row(grads, 0, c), own_at(c), y);
             if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         }
-        const float away = (float)(i0 + see.at - key + 4 * half);
+        const float away = (float)(i0 + from_key);
         to.weights(x, y, [&](int e) { return -of_rows[buffer][0][8 * (e >> 2) + 4 * half + (e & 3)]; },
                    [&](int e) { return away + (float)(8 * (e >> 2) + (e & 3)); });
         if (i0 < all_low || i0 + kStepRows > all_high) {
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-                if ((unsigned)(i0 + 4 * half + 8 * (e >> 2) + (e & 3) - see.lo) >= (unsigned)(see.hi - see.lo)) x[e] = y[e] = 0.f;
+                if ((unsigned)(i0 + from_first + 8 * (e >> 2) + (e & 3)) >= seen) x[e] = y[e] = 0.f;
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -308,16 +325,17 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
             if (wave < 2 && lane < kStepRows) fetch_words(of_rows[to][wave], sums_of(wave, head, i0), lane, last - i0);
         };
         begin();
-        if (first < last) bring(head0, first, 0);
+        if (head0 < head1) bring(head0, row0, 0);
         for (int head = head0; head < head1; ++head) {
-            const Scores to(p, head, true);
-            for (int i0 = first; i0 < last; i0 += kStepRows, buffer ^= 1, at_lane.other(L::kBytes)) {
+            to.of_head(p, head);
+            const int end = head + 1 < head1 ? last : row1;
+            for (int i0 = head == head0 ? row0 : first; i0 < end; i0 += kStepRows, buffer ^= 1, at_lane.other(L::kBytes)) {
                 arrive_and_wait();
-                if (i0 + kStepRows < last)
+                if (i0 + kStepRows < end)
                     bring(head, i0 + kStepRows, buffer ^ 1);
                 else if (head + 1 < head1)
                     bring(head + 1, first, buffer ^ 1);
-                tile_of(to, i0, buffer);
+                tile_of(i0, buffer);
             }
         }
         done = all_finite();
@@ -329,15 +347,15 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     for (; !done; ++entries) {
         begin();
         for (int head = head0; head < head1; ++head) {
-            const Scores to(p, head, true);
-            for (int i0 = first; i0 < last; i0 += kStepRows) {
+            to.of_head(p, head);
+            const int end = head + 1 < head1 ? last : row1;
+            for (int i0 = head == head0 ? row0 : first; i0 < end; i0 += kStepRows) {
                 arrive_and_wait();
                 stage<T, DP, 256, kStepRows>(queries, p.q, head, i0, first, last, p.d, tid, entries);
                 stage<T, DP, 256, kStepRows>(grads, p.dO, head, i0, first, last, p.d, tid, entries);
-                if (wave < 2 && lane < kStepRows)
-                    of_rows[0][wave][lane] = i0 + lane < last ? sums_of(wave, head, i0)[lane] : 0.f;
+                if (wave < 2 && lane < kStepRows) of_rows[0][wave][lane] = i0 + lane < last ? sums_of(wave, head, i0)[lane] : 0.f;
                 arrive_and_wait();
-                tile_of(to, i0, 0);
+                tile_of(i0, 0);
             }
         }
         done = entries == kFinite || all_finite();

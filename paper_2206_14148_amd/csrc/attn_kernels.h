@@ -8,7 +8,8 @@ namespace attn {
 
 constexpr int kTileRows = 128;  // rows of Q (forward, dQ) or keys (dK, dV) per workgroup: 4 waves x 32
 constexpr int kTileKeys = 64;   // keys, or rows, per step of the walk
-constexpr int kMaxSplits = 64;
+constexpr int kStepRows = 32;    // rows per step of the gradient by keys
+constexpr int kMaxSplits = 256;
 
 struct Rows {  // one tensor [rows][heads][d], see attn_rows_t
     unsigned short* data;
