@@ -19,17 +19,34 @@ namespace {
 
 constexpr int64_t kMostRows = (int64_t)1 << 30;
 
-// Workgroups that fill the GPU: two on a compute unit.  Of the kernel by keys one is on a compute unit at a time, its
-// registers are those of two; with a causal mask the first keys' are twice as long as the mean, so that four rounds of
-// shorter ones end sooner than one of long ones, although the parts have to be written and read.
-constexpr int64_t kWantRows = 2 * knn::kNumCU, kWantKeys = 4 * knn::kNumCU;
-// A range of keys is worth a workgroup of its own from this many on (two tiles): 3 rows of 16 heads against 50021 keys took 34 us
-// in ranges of 782 keys and XXX in ranges of 196.  Below kLeastSplit keys the join, a launch of its own, costs more than
-// half the walk.  One part of the gradient by keys has kLeastSteps steps at least.
-constexpr int64_t kLeastRange = 128, kLeastSplit = 512, kLeastSteps = 16;
+// Into how many parts a walk is cut.  What a part costs, measured for bf16 rows of 80 and 128, one to 50021 of them: a step (64
+// keys, or 32 rows by keys) takes 1.15 us where a compute unit has one workgroup and 1.7 times that where two share it; parts have
+// to be written and read at 4 TB/s, and their join is a launch of 5 us.  A workgroup's walk ends no earlier than its
+// own steps, all workgroups' no earlier than 2 to a compute unit allow; `share` is the part of the steps that the mean
+// workgroup has (by keys half, as with a causal mask, where the first keys' workgroups have all).
+// 3 rows of 16 heads against 50021 keys: 854 us in one part, 25 in 256; 1201 rows of 8 heads: 27 in one, 22 in 4, 27 in 8;
+// the gradient of 4096 rows of 32 heads: 1000 in one, 575 in 4.
+int best_parts(int64_t workgroups, int64_t steps, double share, double bytes_a_part, uint64_t room, uint64_t (*bytes)(const int64_t*, int64_t),
+               const int64_t* shape) {
+    int best = 1;
+    double least = 0;
+    for (int64_t s = 1; s <= attn::kMaxSplits && (s == 1 || (steps >= 2 * s && bytes(shape, s) <= room)); s *= 2) {
+        const double each = (double)((steps + s - 1) / s) * 1.15, all = (double)workgroups * s;
+        const double own = each * (all > knn::kNumCU ? 1.7 : 1.0), total = all * each * share * 1.7 / (2 * knn::kNumCU);
+        const double t = (own > total ? own : total) + (s > 1 ? 5.0 + s * bytes_a_part / 4e6 : 0.0);
+        if (s == 1 || t < 0.95 * least) {
+            best = (int)s;
+            least = t;
+        }
+    }
+    return best;
+}
 
-uint64_t part_bytes(int64_t n, int32_t hq, int32_t d, int64_t splits) {
-    return splits > 1 ? knn::align_up((uint64_t)splits * n * hq * (d + 2) * 4) : 0;
+uint64_t row_parts(const int64_t* rows_d, int64_t parts) {  // rows times heads, d
+    return parts > 1 ? knn::align_up((uint64_t)parts * rows_d[0] * (rows_d[1] + 2) * 4) : 0;
+}
+uint64_t key_parts(const int64_t* keys_d, int64_t parts) {  // keys times heads, d: dK and dV
+    return parts > 1 ? knn::align_up((uint64_t)parts * 2 * keys_d[0] * keys_d[1] * 4) : 0;
 }
 
 knn_status check_shape(int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t d, attn_plan_t* out) {
@@ -105,12 +122,10 @@ extern "C" knn_status attn_plan(int64_t n, int64_t m, int32_t hq, int32_t hkv, i
     const knn_status st = check_shape(n, m, hq, hkv, d, out);
     if (st != KNN_OK) return st;
     const int64_t tiles = (n * (hq / hkv) + attn::kTileRows - 1) / attn::kTileRows * hkv;
-    int64_t s = 1;
-    while (m >= kLeastSplit && tiles > 0 && tiles * s < kWantRows && 2 * s <= attn::kMaxSplits && m / (2 * s) >= kLeastRange &&
-           part_bytes(n, hq, d, 2 * s) <= mem_limit_bytes)
-        s *= 2;
-    out->n_splits = (int32_t)s;
-    out->workspace_bytes = part_bytes(n, hq, d, s);
+    const int64_t shape[2] = {n * hq, d};
+    out->n_splits = n == 0 ? 1 : best_parts(tiles, (m + attn::kTileKeys - 1) / attn::kTileKeys, 1.0, 8.0 * n * hq * (d + 2), mem_limit_bytes,
+                                            row_parts, shape);
+    out->workspace_bytes = row_parts(shape, out->n_splits);
     return KNN_OK;
 }
 
@@ -123,13 +138,9 @@ extern "C" knn_status attn_grad_plan(int64_t n, int64_t m, int32_t hq, int32_t h
     if (mem_limit_bytes < sums) return KNN_ERR_MEM_LIMIT_TOO_SMALL;
     const int64_t tiles = (m + attn::kTileRows - 1) / attn::kTileRows * hkv;
     const int64_t steps = (n + attn::kStepRows - 1) / attn::kStepRows * (hq / hkv);
-    auto bytes = [&](int64_t s) { return s > 1 ? knn::align_up((uint64_t)s * 2 * m * hkv * d * 4) : 0; };
-    int64_t s = 1;
-    while (tiles > 0 && tiles * s < kWantKeys && 2 * s <= attn::kMaxSplits && steps / (2 * s) >= kLeastSteps &&
-           sums + bytes(2 * s) <= mem_limit_bytes)
-        s *= 2;
-    out->n_splits = (int32_t)s;
-    out->workspace_bytes = sums + bytes(s);
+    const int64_t shape[2] = {m * hkv, d};
+    out->n_splits = m == 0 ? 1 : best_parts(tiles, steps, 0.5, 16.0 * m * hkv * d, mem_limit_bytes - sums, key_parts, shape);
+    out->workspace_bytes = sums + key_parts(shape, out->n_splits);
     return KNN_OK;
 }
 

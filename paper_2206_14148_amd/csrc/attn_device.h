@@ -108,6 +108,31 @@ __device__ __forceinline__ int document_of(const int* starts, int docs, int x) {
     return low;
 }
 
+// The arrays in LDS where there are few documents, so that the searches, every step of which waits for the one before,
+// do not go to memory (some 4 us a kernel).  All threads of the workgroup, which wait for each other here.
+constexpr int kLocalDocs = 127;
+struct LocalDocs {
+    int starts[kLocalDocs + 1], k_starts[kLocalDocs + 1], prefix[kLocalDocs + 1];
+};
+__device__ __forceinline__ Mask with_local(const Mask& k, LocalDocs& local, int tid) {
+    Mask m = k;
+    if (k.docs > kLocalDocs || !(k.starts || k.prefix)) return m;
+    if (tid <= k.docs) {
+        if (k.starts) {
+            local.starts[tid] = k.starts[tid];
+            local.k_starts[tid] = k.k_starts[tid];
+        }
+        if (k.prefix && tid < k.docs) local.prefix[tid] = k.prefix[tid];
+    }
+    __syncthreads();
+    if (k.starts) {
+        m.starts = local.starts;
+        m.k_starts = local.k_starts;
+    }
+    if (k.prefix) m.prefix = local.prefix;
+    return m;
+}
+
 __device__ __forceinline__ int clamp_to(int64_t x, int low, int high) {
     return x < low ? low : x > high ? high : (int)x;
 }
@@ -353,6 +378,17 @@ __device__ __forceinline__ void put4(unsigned short* p, int c, int d, int wide, 
         if (c + 1 < d) p[c + 1] = (unsigned short)(a >> 16);
         if (c + 2 < d) p[c + 2] = (unsigned short)b;
         if (c + 3 < d) p[c + 3] = (unsigned short)(b >> 16);
+    }
+}
+
+// Numbers e .. e + 3 of x as entries c .. c + 3 of a row of d, 16 bytes at a time where rows are.
+__device__ __forceinline__ void put4(float* p, int c, int d, const f32x16& x, int e) {
+    if (d % 4 == 0) {
+        if (c < d) *reinterpret_cast<f32x4*>(p + c) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < d) p[c + i] = x[e + i];
     }
 }
 

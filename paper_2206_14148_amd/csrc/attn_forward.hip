@@ -36,10 +36,7 @@ __device__ __forceinline__ void write_rows(const Problem& p, const Span& see, in
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int c = 32 * b + 8 * (e >> 2) + 4 * half + (e & 3);
-                if (c < p.d) parts[c] = sum[b][e];
-            }
+            for (int a = 0; a < 4; ++a) put4(parts, 32 * b + 8 * a + 4 * half, p.d, sum[b], 4 * a);
         if (half == 0) {
             float* ends_of = p.partial + (int64_t)p.splits * rows * p.d + 2 * ((int64_t)split * rows + at);
             ends_of[0] = top;
@@ -72,7 +69,8 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     // the last rows first: with a causal mask they see the most keys
     const int split = w % p.splits, tile = tiles - 1 - w / p.splits % tiles, kv = w / p.splits / tiles;
     const int line = tile * kTileRows + wave * 32 + (lane & 31), row = line / group, head = kv * group + line % group;
-    const Span see = keys_of_row(p.mask, row);
+    __shared__ LocalDocs local;
+    const Span see = keys_of_row(with_local(p.mask, local, tid), row);
     const bool some = see.lo < see.hi;
     const int low = wave_least(some ? see.lo : INT_MAX), high = wave_most(some ? see.hi : INT_MIN);
     // keys that all rows of the wave see (rows that are not written do not count)

@@ -60,7 +60,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     const int w = work_of(blockIdx.x, gridDim.x);
     const int tile = tiles - 1 - w % tiles, kv = w / tiles;
     const int line = tile * kTileRows + wave * 32 + (lane & 31), row = line / group, head = kv * group + line % group;
-    const Span see = keys_of_row(p.mask, row);
+    __shared__ LocalDocs local;
+    const Span see = keys_of_row(with_local(p.mask, local, tid), row);
     const bool some = see.lo < see.hi;
     const int low = wave_least(some ? see.lo : INT_MAX), high = wave_most(some ? see.hi : INT_MIN);
     const int all_low = wave_most(see.inside ? see.lo : INT_MIN), all_high = wave_least(see.inside ? see.hi : INT_MAX);
@@ -214,7 +215,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     // the first keys first: with a causal mask most rows see them
     const int part = w % p.splits, tile = w / p.splits % tiles, kv = w / p.splits / tiles;
     const int key = tile * kTileRows + wave * 32 + (lane & 31);
-    const Span see = rows_of_key(p.mask, key);
+    __shared__ LocalDocs local;
+    const Span see = rows_of_key(with_local(p.mask, local, tid), key);
     const bool some = see.lo < see.hi;
     const int low = wave_least(some ? see.lo : INT_MAX), high = wave_most(some ? see.hi : INT_MIN);
     const int all_low = wave_most(see.inside ? see.lo : INT_MIN), all_high = wave_least(see.inside ? see.hi : INT_MAX);
@@ -372,11 +374,9 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int c = 32 * b + 8 * (e >> 2) + 4 * half_again + (e & 3);
-                if (c >= p.d) continue;
-                o[c] = dk[b][e] * p.scale;
-                o[keys * p.d + c] = dv[b][e];
+            for (int a = 0; a < 4; ++a) {
+                put4(o, 32 * b + 8 * a + 4 * half_again, p.d, dk[b] * p.scale, 4 * a);
+                put4(o + keys * p.d, 32 * b + 8 * a + 4 * half_again, p.d, dv[b], 4 * a);
             }
         return;
     }

@@ -118,7 +118,7 @@ def test_work_split_along_the_keys_and_over_the_heads(dtype):
         compare("O", O, r)
         compare("lse", lse, r)
     # parts of the gradient by keys begin and end within a head's rows
-    assert A.attn_grad_plan(300, 300, 8, 1, 64, GB).n_splits == 4 and A.attn_grad_plan(700, 300, 3, 1, 64, GB).n_splits == 4
+    assert A.attn_grad_plan(300, 300, 8, 1, 64, GB).n_splits > 8 and A.attn_grad_plan(700, 300, 3, 1, 64, GB).n_splits > 3
     data = make(300, 300, 8, 1, 64, dtype, 5)
     check(*data, causal=True)
     check(*make(700, 300, 3, 1, 64, dtype, 6), starts=[0, 100, 333, 690], k_starts=[0, 10, 200, 299])

@@ -32,7 +32,7 @@ def test_plans_stay_under_their_limit_and_count_what_they_keep(n, m, hq, hkv, d)
         p = A.attn_plan(n, m, hq, hkv, d, limit)
         assert p.workspace_bytes <= limit and p.min_limit_bytes == 0
         assert p.workspace_bytes == (up(p.n_splits * n * hq * (d + 2) * 4) if p.n_splits > 1 else 0)
-        assert p.n_splits == 1 or m // p.n_splits >= 128
+        assert p.n_splits == 1 or m // p.n_splits >= 64
         least = up(8 * n * hq)
         if limit < least:
             with pytest.raises(A.KnnError) as e:
