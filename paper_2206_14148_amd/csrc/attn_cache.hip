@@ -154,55 +154,68 @@ __device__ __forceinline__ float quotient_of(float code, float from, float to) {
 
 // A workgroup looks at `tokens` new rows for one head; where the first row of a run of rows that go to one block is among
 // them it does the run.  What bounds it for a step's few rows is one memory access waiting for another: slots, then rows and
-// scales, then the codes go out.  Rows are kept in registers from the search of the largest magnitude to the codes where four
-// passes of the workgroup hold them (64 rows of 128), else read again.  A block's codes of V lie across its rows, so they are
-// put together in LDS and written a word of four tokens at a time; a word that the run fills in part, and that is not begun
-// anew, is written byte by byte.
-constexpr int kAppendThreads = 256, kAppendPasses = 4;
-template <typename T, bool E4M3>
-__global__ __launch_bounds__(kAppendThreads) void attn_append_kernel(AppendProblem p, int tokens) {
+// scales, then the codes go out (8 us for one row, 12 for 64 rows and 8 heads, of which a launch is 3).  Blocks of up to 32
+// tokens take a wave, whose lanes need not wait for each other (9216 rows of 128, 8 heads, blocks of 16: 31 us, with four
+// waves 69), larger ones four (64 rows, blocks of 64: 15 us, with one wave 40; 9216 rows 92).  Rows are kept in registers from the
+// search of the largest magnitude to the codes where they fit, else read again.  A block's codes of V lie across its rows, so
+// they are put together in LDS and written a word of four tokens at a time; a word that the run fills in part, and that is not
+// begun anew, is written byte by byte.
+constexpr int kAppendPasses = 4;
+template <typename T, bool E4M3, int THREADS>
+__global__ __launch_bounds__(THREADS) void attn_append_kernel(AppendProblem p, int tokens) {
     const Cache& c = p.cache;
     extern __shared__ __attribute__((aligned(16))) unsigned char turned[];  // [row][block + 4]
     __shared__ int last_of[256];               // the last row of the run that goes to each token, -1: none
-    __shared__ int token_of[kAppendThreads];   // of the run's first rows
+    __shared__ int token_of[THREADS];   // of the run's first rows
     __shared__ unsigned covered[8];            // tokens of the block that the run writes
     __shared__ unsigned char moved_to[2][256];  // what becomes of each code that the block holds
-    __shared__ float of_wave[2][kAppendThreads / 64];
+    __shared__ float of_wave[2][THREADS / 64];
     __shared__ int run_end;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x;
     const int head = blockIdx.x % c.hkv, shift = __builtin_ctz(c.block), pitch = c.block + 4;
     const int64_t group = (int64_t)(blockIdx.x / c.hkv) * tokens, slots = c.blocks << shift;
     auto block_of = [&](int64_t t) {
         const int64_t s = t >= 0 && t < p.count ? p.slots[t] : -1;
         return s >= 0 && s < slots ? s >> shift : -1;
     };
-    // lane l looks at row group + l: whether a run begins there
-    const int64_t mine = lane < tokens ? block_of(group + lane) : -1, before_mine = lane < tokens ? block_of(group + lane - 1) : -1;
+    // lane l of each wave: whether a run begins at row group + l
+    const int64_t mine = (tid & 63) < tokens ? block_of(group + (tid & 63)) : -1;
+    const int64_t before_mine = (tid & 63) < tokens ? block_of(group + (tid & 63) - 1) : -1;
     unsigned long long firsts = __ballot(mine >= 0 && mine != before_mine);
-    const int pieces = c.row / 8, per_pass = kAppendThreads / pieces, piece = tid % pieces, line = tid / pieces;
+    const int pieces = c.row / 8, per_pass = THREADS / pieces, piece = tid % pieces, line = tid / pieces;
     while (firsts) {
         const int64_t first = group + __builtin_ctzll(firsts), block = block_of(first), at = block * c.hkv + head;
         firsts &= firsts - 1;
         __syncthreads();
         if (tid < 8) covered[tid] = 0;
-        last_of[tid] = -1;
         if (tid == 0) run_end = INT_MAX;
+        for (int i = tid; i < c.block; i += THREADS) last_of[i] = -1;
         const float scales[2] = {c.k_scale[at], c.v_scale[at]};
         __syncthreads();
         int count = 0;  // rows of the run (slots may be given twice: it can be longer than a block)
-        for (;; count += kAppendThreads) {
+        for (;; count += THREADS) {
             const int64_t t = first + count + tid;
-            if (block_of(t) != block)
-                atomicMin(&run_end, count + tid);
-            else if (count == 0)
-                token_of[tid] = (int)(p.slots[t] & (c.block - 1));
-            __syncthreads();
-            const int found = run_end;
-            __syncthreads();
-            if (found != INT_MAX) break;
+            const bool other = block_of(t) != block;
+            if (count == 0 && !other) token_of[tid] = (int)(p.slots[t] & (c.block - 1));
+            if constexpr (THREADS == 64) {
+                const unsigned long long others = __ballot(other);
+                if (others) {
+                    count += __builtin_ctzll(others);
+                    break;
+                }
+            } else {
+                if (other) atomicMin(&run_end, count + tid);
+                __syncthreads();
+                const int found = run_end;
+                __syncthreads();  // (before anyone lowers it again)
+                if (found != INT_MAX) {
+                    count = found;
+                    break;
+                }
+            }
         }
-        count = run_end;
-        auto token = [&](int i) { return i < kAppendThreads ? token_of[i] : (int)(p.slots[first + i] & (c.block - 1)); };
+        __syncthreads();
+        auto token = [&](int i) { return i < THREADS ? token_of[i] : (int)(p.slots[first + i] & (c.block - 1)); };
         u32x4 rows[2][kAppendPasses];
         auto read = [&](int i0) {
 #pragma unroll
@@ -219,7 +232,7 @@ __global__ __launch_bounds__(kAppendThreads) void attn_append_kernel(AppendProbl
         const int round = kAppendPasses * per_pass;
         for (int i0 = 0; i0 < count; i0 += round) {
             read(i0);
-            for (int i = i0 + tid; i < min(i0 + round, count); i += kAppendThreads) {
+            for (int i = i0 + tid; i < min(i0 + round, count); i += THREADS) {
                 const int to = token(i);
                 atomicOr(&covered[to >> 5], 1u << (to & 31));
                 atomicMax(&last_of[to], i);
@@ -237,34 +250,36 @@ __global__ __launch_bounds__(kAppendThreads) void attn_append_kernel(AppendProbl
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             for (int s = 32; s; s >>= 1) a[x] = fmaxf(a[x], __shfl_xor(a[x], s));
-            if (lane == 0) of_wave[x][wave] = a[x];
+            if (tid % 64 == 0) of_wave[x][tid / 64] = a[x];
         }
         __syncthreads();
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            for (int w = 0; w < THREADS / 64; ++w) a[x] = fmaxf(a[x], of_wave[x][w]);
         const bool fresh = covered[0] & 1;  // token 0: begun anew
         float after[2];
         bool moves[2];
         for (int x = 0; x < 2; ++x) {
-            float largest = 0.f;
-            for (int w = 0; w < kAppendThreads / 64; ++w) largest = fmaxf(largest, of_wave[x][w]);
             const float before = fresh ? 0.f : scales[x];
-            after[x] = fmaxf(before, largest / (E4M3 ? 448.f : 127.f));
+            after[x] = fmaxf(before, a[x] / (E4M3 ? 448.f : 127.f));
             if (tid == 0) (x ? c.v_scale : c.k_scale)[at] = after[x];
             moves[x] = !fresh && after[x] > before;  // codes that the block holds follow its scale
             if (moves[x])
-                moved_to[x][tid] = before > 0.f ? (unsigned char)code_of<E4M3>(quotient_of(value_of<E4M3>(tid), before, after[x])) : 0;
+                for (int i = tid; i < 256; i += THREADS)
+                    moved_to[x][i] = before > 0.f ? (unsigned char)code_of<E4M3>(quotient_of(value_of<E4M3>(i), before, after[x])) : 0;
         }
         if (moves[0] || moves[1]) {
             __syncthreads();
             for (int x = 0; x < 2; ++x) {
                 if (!moves[x]) continue;
                 unsigned* const codes = reinterpret_cast<unsigned*>((x ? c.v : c.k) + at * (int64_t)c.block * c.row);
-                for (int i = tid; i < c.block * c.row / 4; i += kAppendThreads) {
+                for (int i = tid; i < c.block * c.row / 4; i += THREADS) {
                     const unsigned w = codes[i];
                     codes[i] = moved_to[x][w & 255] | moved_to[x][w >> 8 & 255] << 8 | moved_to[x][w >> 16 & 255] << 16 |
                                (unsigned)moved_to[x][w >> 24] << 24;
                 }
             }
-            // other waves write the new codes into those words: the stores have to be done, not only begun (a fence for
+            // other lanes write the new codes into those words: the stores have to be done, not only begun (a fence for
             // the whole device would write the L2 back, 40 us)
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_waitcnt(0);
@@ -316,9 +331,9 @@ __global__ __launch_bounds__(kAppendThreads) void attn_append_kernel(AppendProbl
             }
         }
         __syncthreads();
-        for (int i = tid; i < c.block * c.row / 4; i += kAppendThreads) {
+        for (int i = tid; i < c.block * c.row / 4; i += THREADS) {
             if (fresh) {
-                const int to = 4 * i / c.row;
+                const int to = 4 * i >> (c.row == 64 ? 6 : 7);
                 if (!(covered[to >> 5] >> (to & 31) & 1)) reinterpret_cast<unsigned*>(k_codes)[i] = 0;
             }
             const int to = 4 * i & (c.block - 1), column = 4 * i >> shift;
@@ -635,16 +650,24 @@ hipError_t launch_map(const MapProblem& p, hipStream_t stream) {
     return hipGetLastError();
 }
 
-hipError_t launch_append(const AppendProblem& p, hipStream_t stream) {
-    // A workgroup for each row and head where few rows are each likely to go to a block of their own (a step's); where
-    // there are many, most go where the row before went, and a workgroup looks at as many as the smallest block holds.
-    const int tokens = p.count * p.cache.hkv <= 4096 ? 1 : 16;
-    const dim3 grid((unsigned)((p.count + tokens - 1) / tokens * p.cache.hkv)), block(kAppendThreads);
+namespace {
+template <int THREADS>
+hipError_t append_in(const AppendProblem& p, int tokens, hipStream_t stream) {
+    const dim3 grid((unsigned)((p.count + tokens - 1) / tokens * p.cache.hkv)), block(THREADS);
     const size_t lds = (size_t)p.cache.row * (p.cache.block + 4);
-    auto kernel = p.f16 ? (p.cache.e4m3 ? attn_append_kernel<F16, true> : attn_append_kernel<F16, false>)
-                        : (p.cache.e4m3 ? attn_append_kernel<Bf16, true> : attn_append_kernel<Bf16, false>);
+    auto kernel = p.f16 ? (p.cache.e4m3 ? attn_append_kernel<F16, true, THREADS> : attn_append_kernel<F16, false, THREADS>)
+                        : (p.cache.e4m3 ? attn_append_kernel<Bf16, true, THREADS> : attn_append_kernel<Bf16, false, THREADS>);
     kernel<<<grid, block, lds, stream>>>(p, tokens);
     return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_append(const AppendProblem& p, hipStream_t stream) {
+    // A step's few rows each go to a block of their own: a workgroup for each row and head.  Of many rows most go where the row
+    // before went, and a workgroup looks at up to as many as the smallest block holds: fewer that find nothing to do.
+    const int64_t all = p.count * p.cache.hkv;
+    const int tokens = all <= 4096 ? 1 : all <= 32768 ? 4 : 16;
+    return p.cache.block <= 32 ? append_in<64>(p, tokens, stream) : append_in<256>(p, tokens, stream);
 }
 
 hipError_t launch_cache(const CacheProblem& p, hipStream_t stream) {
