@@ -40,7 +40,8 @@ typedef enum { ATTN_BF16 = 0, ATTN_F16 = 1 } attn_dtype;
 
 /*
  * A DEVICE tensor [rows][heads][d]: entry t of row i of head h is at data + i * ld + h * hs + t
- * (elements).  ld, hs >= 0; an output's entries must not overlap each other or an input.
+ * (elements).  ld, hs >= 0, of an output >= d where there are several rows (heads); an output's entries must not
+ * overlap each other or an input.
  * Rows are read 16 bytes at a time where data is 16-byte aligned and d, ld and hs are multiples
  * of 8; otherwise entry by entry, which is slower and gives the same results.
  */
@@ -52,8 +53,8 @@ typedef struct {
 typedef struct {
     int32_t dtype;            /* attn_dtype */
     int32_t causal;           /* 0 or 1 */
-    double scale;             /* > 0, finite */
-    double cap;               /* 0: none; else > 0, finite */
+    double scale;             /* 2^-60 .. 2^60 */
+    double cap;               /* 0: none; else 2^-60 .. 2^60 */
     const float *slopes;      /* DEVICE [hq], finite; NULL: none.  Not differentiated */
     int64_t docs;             /* >= 1 with starts; without starts there is one document */
     const int32_t *starts;    /* DEVICE [docs + 1], ascending, within 0 .. n; NULL: 0, n */
@@ -62,11 +63,11 @@ typedef struct {
 } attn_options_t;
 
 /*
- * The plan.  One workgroup owns tile_rows rows of one head and walks the keys; where that leaves
- * compute units idle and the limit has room, the keys are cut into n_splits ranges walked
- * concurrently, whose unnormalised sums, maxima and totals (fp32) lie in the workspace until a last
- * kernel joins them in ascending range order.  The gradient keeps two fp32 numbers per row and head
- * (the row sums of dO * O, the log-sums), and cuts the heads that share a K and V into n_splits parts likewise.
+ * The plan.  One workgroup owns tile_rows rows (of all heads that share a K and V, side by side) and walks
+ * the keys; where that leaves compute units idle and the limit has room, the keys are cut into n_splits
+ * ranges walked concurrently, whose unnormalised sums, maxima and totals (fp32) lie in the workspace until a
+ * last kernel joins them in ascending range order.  The gradient keeps two fp32 numbers per row and head (the row
+ * sums of dO * O, the log-sums), and for dK and dV cuts the rows of all heads that read them into n_splits parts likewise.
  * Results differ between limits that give different n_splits by the rounding of those sums.
  */
 typedef struct {
@@ -97,8 +98,8 @@ knn_status attn_grad_plan(int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t
  *   O [n][hq][d]                     DEVICE out
  *   lse [hq][n]                      DEVICE out, fp32, contiguous (natural logarithm); NULL: not wanted
  *   hip_stream  hipStream_t (NULL: default stream); the call only enqueues work and allocates nothing.
- * Rows before the first document or behind the last are neither read nor written, keys there are not
- * read.  Scores, maxima, totals and sums are fp32; a tile's probabilities are rounded to the type of V
+ * Rows before the first document or behind the last are not written; what they and keys there hold has no
+ * influence.  Scores, maxima, totals and sums are fp32; a tile's probabilities are rounded to the type of V
  * for their product with it, and O is rounded once.  Every sum has a fixed order.
  * An entry that is not finite (NaN in Q; infinite or NaN in K or V) reaches the rows that see it and
  * no others.  A row whose scores are all -infinity counts as one that sees no key.
@@ -119,6 +120,8 @@ knn_status attn_apply(const attn_rows_t *Q, const attn_rows_t *K, const attn_row
  * Rows and keys outside the documents are left as they were.  P and ds are rounded to the type of Q for
  * the products, whose sums are fp32 in a fixed order: no atomics, the same bits on every call.
  * An entry that is not finite makes the gradients not finite of the rows and keys that it meets, and no others.
+ * How exact: P is made from lse, which holds a score to 2^-24 of itself; <dO, O> takes the O that attn_apply rounded, so
+ * where one key has nearly all of a row's weight its ds, a small difference, is off by that rounding.
  */
 knn_status attn_grad(const attn_rows_t *Q, const attn_rows_t *K, const attn_rows_t *V, const attn_rows_t *O,
                      const float *lse, const attn_rows_t *dO, int64_t n, int64_t m, int32_t hq, int32_t hkv,
@@ -166,7 +169,7 @@ int32_t attn_cache_row(int32_t d);
  *   used [1]               DEVICE out, int32: how many entries of `free` the step needs (more than n_free: too few)
  * Lengths beyond width * block, and negative ones, are taken as the nearest that fits; news likewise.  Calling
  * again with the same inputs writes the same.  batch <= 16384.  Errors: KNN_ERR_INVALID_ARG, KNN_ERR_UNSUPPORTED
- * (batch, or width * block above 2^30), KNN_ERR_HIP.
+ * (batch, or width * block above 2^30), KNN_ERR_HIP.  (Sums of lengths beyond 2^31 - 1 are taken as that.)
  */
 knn_status attn_cache_map(const int32_t *lengths, const int32_t *news, int64_t batch, int32_t *table, int64_t width,
                           int32_t block, const int32_t *free, int64_t n_free, int32_t *starts, int64_t *slots,
@@ -181,7 +184,7 @@ knn_status attn_cache_map(const int32_t *lengths, const int32_t *news, int64_t b
  * A new code is the nearest to x / scale' (of two as near the even one; quotients of real numbers).
  * NaN becomes 0 and an infinity the largest code; neither counts for a.
  * The slots of one block must stand together in `slots`, in any order; of a slot given twice the last counts.
- * Where one block's slots stand apart, what becomes of that block is not defined.
+ * Where one block's slots stand apart, what becomes of that block is not defined.  At most 2^27 rows times heads.
  */
 knn_status attn_cache_append(const attn_cache_t *cache, int32_t dtype, const attn_rows_t *K, const attn_rows_t *V,
                              int64_t count, const int64_t *slots, void *hip_stream);

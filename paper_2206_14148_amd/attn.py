@@ -180,6 +180,7 @@ def _dtype(Q):
 
 
 def _shape(Q, K, V):
+    _dtype(Q)
     if Q.dim() != 3 or K.dim() != 3 or V.dim() != 3:
         _refuse("Q, K and V must be [rows, heads, d]")
     (n, hq, d), (m, hkv, _) = Q.shape, K.shape
@@ -231,9 +232,9 @@ def attn_apply(Q, K, V, mem_limit_bytes: int, scale=None, causal: bool = False, 
     documents keep what `out` (O, lse) holds there.  The workspace (uint8, attn_plan's bytes) is
     allocated here unless given.  Work is enqueued on torch's current stream; no synchronisation is done.
     """
-    options = _options(Q, scale, causal, cap, slopes, starts, k_starts, prefix)
     n, m, hq, hkv, d = _shape(Q, K, V)
     plan = _planned(_load().attn_plan, AttnPlanStruct(), n, m, hq, hkv, d, mem_limit_bytes)
+    options = _options(Q, scale, causal, cap, slopes, starts, k_starts, prefix)
     with _on(Q.device):
         workspace, ws, ws_bytes = _workspace(workspace, plan.workspace_bytes, Q.device)
         if out is None:
@@ -265,12 +266,12 @@ def attn_grad(Q, K, V, O, lse, dO, mem_limit_bytes: int, scale=None, causal: boo
     options.  Heads that share a K and V add up.  The workspace (uint8, attn_grad_plan's bytes) is allocated here
     unless given; `out` takes the three gradients.  The same inputs give the same bits.
     """
-    options = _options(Q, scale, causal, cap, slopes, starts, k_starts, prefix)
     n, m, hq, hkv, d = _shape(Q, K, V)
     _check_rows("O", O, Q, (n, hq, d))
     _check_rows("dO", dO, Q, (n, hq, d))
     _check_lse(lse, hq, n, Q.device)
     plan = _planned(_load().attn_grad_plan, AttnPlanStruct(), n, m, hq, hkv, d, mem_limit_bytes)
+    options = _options(Q, scale, causal, cap, slopes, starts, k_starts, prefix)
     with _on(Q.device):
         workspace, ws, ws_bytes = _workspace(workspace, plan.workspace_bytes, Q.device)
         if out is None:

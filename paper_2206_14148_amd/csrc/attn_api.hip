@@ -1,7 +1,6 @@
 // C ABI of the attention product, its gradient and its cache (see include/attn.h for the contract).
 #include <hip/hip_runtime.h>
 
-#include <cmath>
 #include <cstring>
 
 #include "../../include/attn.h"
@@ -76,6 +75,14 @@ bool usable(const attn_rows_t* t, int64_t rows) {
     return rows == 0 || t->data;
 }
 
+// An output: no two of its entries may be one.  (Rows or heads closer than d would be, wherever there are two.)
+bool writable(const attn_rows_t* t, int64_t rows, int32_t heads, int32_t d) {
+    return usable(t, rows) && (rows <= 1 || t->ld >= d) && (heads == 1 || t->hs >= d);
+}
+
+// 0 (a cap: none) or a number that 32 bits, its inverse and its quotients with another one hold with room to spare
+bool ordinary(double x) { return x >= 0x1p-60 && x <= 0x1p60; }
+
 attn::Rows rows_of(const attn_rows_t* t, int32_t d) {
     attn::Rows r;
     r.data = static_cast<unsigned short*>(t->data);
@@ -88,7 +95,7 @@ attn::Rows rows_of(const attn_rows_t* t, int32_t d) {
 
 knn_status fill_problem(const attn_options_t* o, int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t d, attn::Problem* p) {
     if (!o || (o->dtype != ATTN_BF16 && o->dtype != ATTN_F16) || (o->causal != 0 && o->causal != 1)) return KNN_ERR_INVALID_ARG;
-    if (!(o->scale > 0.0) || !std::isfinite(o->scale) || !(o->cap >= 0.0) || !std::isfinite(o->cap)) return KNN_ERR_INVALID_ARG;
+    if (!ordinary(o->scale) || (o->cap != 0.0 && !ordinary(o->cap))) return KNN_ERR_INVALID_ARG;
     if ((o->starts == nullptr) != (o->k_starts == nullptr)) return KNN_ERR_INVALID_ARG;
     if (o->starts ? o->docs < 1 || o->docs >= ((int64_t)1 << 31) - 1 : o->docs != 0 && o->docs != 1) return KNN_ERR_INVALID_ARG;
     std::memset(p, 0, sizeof(*p));
@@ -155,7 +162,7 @@ extern "C" knn_status attn_apply(const attn_rows_t* Q, const attn_rows_t* K, con
     attn::Problem p;
     st = fill_problem(options, n, m, hq, hkv, d, &p);
     if (st != KNN_OK) return st;
-    if (!usable(Q, n) || !usable(K, m) || !usable(V, m) || !usable(O, n)) return KNN_ERR_INVALID_ARG;
+    if (!usable(Q, n) || !usable(K, m) || !usable(V, m) || !writable(O, n, hq, d)) return KNN_ERR_INVALID_ARG;
     if (n == 0) return KNN_OK;
     st = check_workspace(plan, workspace, workspace_bytes);
     if (st != KNN_OK) return st;
@@ -188,8 +195,8 @@ extern "C" knn_status attn_grad(const attn_rows_t* Q, const attn_rows_t* K, cons
     attn::Problem p;
     st = fill_problem(options, n, m, hq, hkv, d, &p);
     if (st != KNN_OK) return st;
-    if (!usable(Q, n) || !usable(K, m) || !usable(V, m) || !usable(O, n) || !usable(dO, n) || !usable(dQ, n) ||
-        !usable(dK, m) || !usable(dV, m) || (n > 0 && !lse))
+    if (!usable(Q, n) || !usable(K, m) || !usable(V, m) || !usable(O, n) || !usable(dO, n) ||
+        !writable(dQ, n, hq, d) || !writable(dK, m, hkv, d) || !writable(dV, m, hkv, d) || (n > 0 && !lse))
         return KNN_ERR_INVALID_ARG;
     if (n == 0 && m == 0) return KNN_OK;
     st = check_workspace(plan, workspace, workspace_bytes);
@@ -281,7 +288,7 @@ extern "C" knn_status attn_cache_append(const attn_cache_t* cache, int32_t dtype
     attn::AppendProblem p;
     if (!cache_of(cache, &p.cache) || (dtype != ATTN_BF16 && dtype != ATTN_F16) || count < 0) return KNN_ERR_INVALID_ARG;
     if (!usable(K, count) || !usable(V, count) || (count > 0 && !slots)) return KNN_ERR_INVALID_ARG;
-    if (count > kMostRows || count * cache->hkv > ((int64_t)1 << 32)) return KNN_ERR_UNSUPPORTED;
+    if (count > kMostRows || count * cache->hkv > ((int64_t)1 << 27)) return KNN_ERR_UNSUPPORTED;
     if (count == 0 || cache->blocks == 0) return KNN_OK;
     p.k = rows_of(K, cache->d);
     p.v = rows_of(V, cache->d);
@@ -299,7 +306,7 @@ extern "C" knn_status attn_cache_plan(int64_t batch, int32_t nq, int32_t hq, int
     if (batch < 0 || longest < 0 || nq < 1 || hkv < 1 || hq < hkv || hq % hkv != 0 || d < 1) return KNN_ERR_INVALID_ARG;
     if (d > ATTN_MAX_D || longest > kMostRows || batch > kMostRows || hq > 65535 || nq > 65535) return KNN_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)nq * (hq / hkv), per = rows > 16 ? 32 : 16;
-    if ((double)batch * hkv * ((rows + per - 1) / per) > (1 << 24)) return KNN_ERR_UNSUPPORTED;
+    if ((double)batch * hkv * ((rows + per - 1) / per) >= (1 << 24)) return KNN_ERR_UNSUPPORTED;
     const int64_t sets = batch * hkv * ((rows + per - 1) / per);
     auto bytes = [&](int64_t ranges) {
         return ranges > 1 ? knn::align_up((uint64_t)ranges * batch * nq * hq * (d + 2) * 4) : 0;
@@ -328,12 +335,12 @@ extern "C" knn_status attn_cache_apply(const attn_cache_t* cache, int32_t dtype,
                                        const attn_rows_t* O, void* hip_stream) {
     attn::CacheProblem p;
     if (!cache_of(cache, &p.cache) || (dtype != ATTN_BF16 && dtype != ATTN_F16) || width < 0) return KNN_ERR_INVALID_ARG;
-    if (!(scale > 0.0) || !std::isfinite(scale) || !(cap >= 0.0) || !std::isfinite(cap)) return KNN_ERR_INVALID_ARG;
+    if (!ordinary(scale) || (cap != 0.0 && !ordinary(cap))) return KNN_ERR_INVALID_ARG;
     if (width > kMostRows / cache->block) return KNN_ERR_UNSUPPORTED;
     attn_cache_plan_t plan;
     const knn_status st = attn_cache_plan(batch, nq, hq, cache->hkv, cache->d, width * cache->block, mem_limit_bytes, &plan);
     if (st != KNN_OK) return st;
-    if (!usable(Q, batch) || !usable(O, batch) || (batch > 0 && !lengths) || (batch > 0 && width > 0 && !table))
+    if (!usable(Q, batch) || !writable(O, batch * nq, hq, cache->d) || (batch > 0 && !lengths) || (batch > 0 && width > 0 && !table))
         return KNN_ERR_INVALID_ARG;
     if (batch == 0) return KNN_OK;
     if (plan.workspace_bytes > 0) {

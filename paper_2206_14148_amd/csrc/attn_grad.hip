@@ -200,8 +200,10 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
 }
 
 // By keys a step takes 32 rows, and V, the second operand of only one product, stays in LDS: so two workgroups share a
-// compute unit, one's exponentials beside the other's products (with V in registers and 64 rows a step: one, and 444 us in
-// place of XXX at 4096 rows and keys, 32 heads on 8, d = 128).
+// compute unit, one's exponentials beside the other's products.  4096 rows and keys, causal, 32 heads on 8, d = 128, bf16: 345 us
+// or 800 TFLOP/s of its four products (with V in registers and 64 rows a step one workgroup, and 444 us); the walk by rows
+// takes 245 us for its three, 840 TFLOP/s.  What bounds both is the matrix cores' share: the vector instructions of the
+// exponentials (some 10 for a score) take nearly as long as the products, and hide behind the other workgroup's only in part.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     typedef Tile<DP, kStepRows> L;

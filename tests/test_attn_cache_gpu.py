@@ -335,3 +335,56 @@ def test_a_service_step_by_step_and_as_a_graph():
         O, most = F.cache_attention(q1, *codes, want[0], lengths, d, block, cap=30.0)
         assert ((got.double().cpu() - O).abs() <= most).all()
         free = free[want[3]:]
+
+
+def test_a_cache_beyond_32_bits():
+    """Blocks whose codes lie more than 2^32 bytes into the cache."""
+    d, hq, hkv, block, blocks = 128, 8, 8, 64, 66_000
+    big = A.AttnCache.empty(blocks, hkv, d, block, "int8")
+    assert big.k.numel() > 1 << 32
+    gen = torch.Generator().manual_seed(1)
+    K, V = (torch.randn(130, hkv, d, generator=gen).half().cuda() for _ in range(2))
+    small = A.AttnCache.empty(3, hkv, d, block, "int8")
+    A.attn_cache_append(small, K, V, torch.arange(130, device="cuda"))
+    A.attn_cache_append(big, K, V, torch.arange(130, device="cuda") + (blocks - 3) * block)
+    for a, b in ((small.k, big.k), (small.v, big.v), (small.k_scale, big.k_scale), (small.v_scale, big.v_scale)):
+        assert torch.equal(a, b[-3:]) and not b[:4].any()
+    Q = torch.randn(1, 1, hq, d, generator=gen).half().cuda()
+    want = A.attn_cache_apply(Q, small, words([[0, 1, 2]]), words([130]), GB)
+    got = A.attn_cache_apply(Q, big, words([[blocks - 3, blocks - 2, blocks - 1]]), words([130]), GB)
+    assert torch.equal(got, want)
+
+
+def test_gpu_refusals():
+    cache = A.AttnCache.empty(4, 2, 64, 16, "int8")
+    K = torch.zeros(3, 2, 64, dtype=torch.half, device="cuda")
+    slots = torch.arange(3, device="cuda")
+    Q = torch.zeros(2, 1, 4, 64, dtype=torch.half, device="cuda")
+    table, lengths = words([[0], [1]]), words([3, 2])
+
+    def refused(f):
+        with pytest.raises(A.KnnError) as e:
+            f()
+        assert e.value.status == A.KNN_ERR_INVALID_ARG, e.value
+
+    refused(lambda: A.attn_cache_append(cache, K.float(), K.float(), slots))
+    refused(lambda: A.attn_cache_append(cache, K, K[:2], slots))
+    refused(lambda: A.attn_cache_append(cache, K, K, slots.int()))
+    refused(lambda: A.attn_cache_append(cache, K, K, slots[:2]))
+    refused(lambda: A.attn_cache_append(cache, K[:, :1], K[:, :1], slots))
+    refused(lambda: A.attn_cache_append(A.AttnCache(cache.k, cache.k, cache.k_scale, cache.v_scale, 64), K, K, slots))
+    refused(lambda: A.attn_cache_append(A.AttnCache(cache.k.float(), cache.v, cache.k_scale, cache.v_scale, 64), K, K, slots))
+    refused(lambda: A.attn_cache_append(A.AttnCache(cache.k, cache.v, cache.k_scale.half(), cache.v_scale, 64), K, K, slots))
+    refused(lambda: A.attn_cache_append(A.AttnCache(cache.k, cache.v, cache.k_scale, cache.v_scale, 65), K, K, slots))
+    refused(lambda: A.attn_cache_apply(Q, cache, table.long(), lengths, GB))
+    refused(lambda: A.attn_cache_apply(Q, cache, table[:1], lengths, GB))
+    refused(lambda: A.attn_cache_apply(Q, cache, table, lengths[:1], GB))
+    refused(lambda: A.attn_cache_apply(Q[0], cache, table, lengths, GB))
+    refused(lambda: A.attn_cache_apply(Q[:, :, :3], cache, table, lengths, GB))
+    refused(lambda: A.attn_cache_apply(Q, cache, table, lengths, GB, slopes=torch.ones(3, device="cuda")))
+    refused(lambda: A.attn_cache_apply(Q, cache, table, lengths, GB, out=Q.float()))
+    refused(lambda: A.attn_cache_apply(Q, cache, table, lengths, GB, scale=-1.0))
+    refused(lambda: A.attn_cache_map(lengths.cpu(), lengths, table, lengths, 16, 4))
+    refused(lambda: A.attn_cache_map(lengths, lengths[:1], table, lengths, 16, 4))
+    refused(lambda: A.attn_cache_map(lengths, lengths, table, lengths.long(), 16, 4))
+    refused(lambda: A.attn_cache_map(lengths, lengths, table, lengths, 17, 4))

@@ -284,3 +284,65 @@ def test_same_bits_other_streams_and_captured_graphs():
         for t, w in zip(got + got_few, want + few):
             assert torch.equal(t, w)
         ws.fill_(255)
+
+
+def test_rows_far_apart_in_memory():
+    """Offsets beyond 32 bits: rows of a very wide matrix, at both ways of reading them, and rows very far apart."""
+    d, hq, hkv = 64, 2, 1
+    big = torch.zeros(1 << 32, dtype=torch.int8, device="cuda").view(torch.bfloat16)  # 2^31 entries
+    big = torch.cat([big, big[: 1 << 27]])
+    for n, ld, shift in ((50_000, 44_000, 0), (50_000, 44_000, 1), (17, 1 << 27, 0)):
+        base = torch.as_strided(big, (n, hkv, d), (ld, d, 1), shift)
+        small = make(40, n, hq, hkv, d, "bf16", 3)
+        base.copy_(small[1])
+        starts, k_starts = [0, 40], [max(0, n - 300), n]
+        o = dict(causal=True, starts=words(starts), k_starts=words(k_starts))
+        want = A.attn_apply(*small[:3], GB, **o)
+        got = A.attn_apply(small[0], base, small[2], GB, **o)
+        for g, w in zip(got, want):
+            assert torch.equal(g, w)
+        grads = A.attn_grad(*small[:3], *want, small[3], GB, **o)
+        out = [torch.empty_like(small[0]), base, torch.empty_like(small[2])]
+        got = A.attn_grad(*small[:3], *want, small[3], GB, out=out, **o)
+        assert torch.equal(got[0], grads[0])
+        for g, w in zip(got[1:], grads[1:]):
+            assert torch.equal(g[k_starts[0]:], w[k_starts[0]:])
+        base.zero_()
+
+
+def test_gpu_refusals():
+    Q, K, V, dO = make(8, 9, 4, 2, 64, "bf16", 2)
+
+    def refused(f):
+        with pytest.raises(A.KnnError) as e:
+            f()
+        assert e.value.status == A.KNN_ERR_INVALID_ARG, e.value
+
+    refused(lambda: A.attn_apply(Q, K.half(), V, GB))
+    refused(lambda: A.attn_apply(Q.float(), K.float(), V.float(), GB))
+    refused(lambda: A.attn_apply(Q, K, V[:5], GB))
+    refused(lambda: A.attn_apply(Q[0], K, V, GB))
+    refused(lambda: A.attn_apply(Q[:, :, ::2], K[:, :, ::2], V[:, :, ::2], GB))
+    refused(lambda: A.attn_apply(Q, K.cpu(), V, GB))
+    refused(lambda: A.attn_apply(Q[:, :3], K, V, GB))
+    refused(lambda: A.attn_apply(Q, K, V, GB, slopes=torch.ones(3, device="cuda")))
+    refused(lambda: A.attn_apply(Q, K, V, GB, slopes=torch.ones(4)))
+    refused(lambda: A.attn_apply(Q, K, V, GB, starts=words([0, 8]).long()))
+    refused(lambda: A.attn_apply(Q, K, V, GB, starts=words([0, 8]), k_starts=words([0, 4, 9])))
+    refused(lambda: A.attn_apply(Q, K, V, GB, k_starts=words([0, 9])))
+    refused(lambda: A.attn_apply(Q, K, V, GB, starts=words([0])))
+    refused(lambda: A.attn_apply(Q, K, V, GB, prefix=words([1, 2])))
+    refused(lambda: A.attn_apply(Q, K, V, GB, scale=0.0))
+    refused(lambda: A.attn_apply(Q, K, V, GB, cap=-1.0))
+    lse = torch.empty(4, 8, device="cuda")
+    refused(lambda: A.attn_apply(Q, K, V, GB, out=(torch.empty_like(Q)[:, :1].expand(Q.shape), lse)))
+    refused(lambda: A.attn_apply(Q, K, V, GB, out=(torch.empty_like(Q), lse.T)))
+    refused(lambda: A.attn_apply(Q, K, V, GB, workspace=torch.empty(10, device="cuda")))
+    refused(lambda: A.attn_grad(Q, K, V, Q, lse.double(), dO, GB))
+    refused(lambda: A.attn_grad(Q, K, V, Q, lse, dO[:4], GB))
+    with pytest.raises(A.KnnError) as e:
+        A.attn_grad(Q, K, V, Q, lse, dO, 10)
+    assert e.value.status == A.KNN_ERR_MEM_LIMIT_TOO_SMALL and e.value.min_limit_bytes == 256
+    with pytest.raises(A.KnnError) as e:
+        A.attn_grad(Q, K, V, Q, lse, dO, GB, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == A.KNN_ERR_WORKSPACE_TOO_SMALL

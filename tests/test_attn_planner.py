@@ -81,6 +81,7 @@ def test_calls_that_are_refused():
            dict(scale=float("inf")), dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(starts=0x1000),
            dict(k_starts=0x1000), dict(docs=2), dict(starts=0x1000, k_starts=0x1000, docs=0),
            dict(starts=0x1000, k_starts=0x1000, docs=1 << 31)]
+    bad += [dict(scale=1e-30), dict(scale=1e30), dict(cap=1e-30), dict(cap=1e30)]
     null, backward = attn.RowsStruct(None, 128, 64), attn.RowsStruct(0x1000, -1, 64)
     for grad in (False, True):
         for o in bad:
@@ -89,6 +90,10 @@ def test_calls_that_are_refused():
             assert call(grad=grad, **{name: null}) == A.KNN_ERR_INVALID_ARG
             assert call(grad=grad, **{name: backward}) == A.KNN_ERR_INVALID_ARG
         assert call(d=129, grad=grad) == A.KNN_ERR_UNSUPPORTED
+        for name in ("dq", "dk", "dv") if grad else ("out",):  # outputs whose rows or heads lie on each other
+            heads = 1 if name in ("dk", "dv") else 2
+            assert call(grad=grad, **{name: attn.RowsStruct(0x1000, 63, 64)}) == A.KNN_ERR_INVALID_ARG
+            assert heads == 1 or call(grad=grad, **{name: attn.RowsStruct(0x1000, 128, 0)}) == A.KNN_ERR_INVALID_ARG
     # few rows, many keys: parts in the workspace
     assert call(m=100_000, ws=None) == A.KNN_ERR_INVALID_ARG
     assert call(m=100_000, ws=0x1001) == A.KNN_ERR_INVALID_ARG
@@ -189,7 +194,9 @@ def test_cache_calls_that_are_refused():
     assert apply(dtype=2) == bad and apply(q=null) == bad and apply(out=null) == bad and apply(table=None) == bad
     assert apply(lengths=None) == bad and apply(scale=0.0) == bad and apply(scale=float("nan")) == bad and apply(cap=-1.0) == bad
     assert apply(hq=3) == bad and apply(nq=0) == bad and apply(batch=-1) == bad and apply(width=-1) == bad
-    assert apply(width=1 << 28) == A.KNN_ERR_UNSUPPORTED
+    assert apply(width=1 << 28) == A.KNN_ERR_UNSUPPORTED and append(count=1 << 27) == A.KNN_ERR_UNSUPPORTED
+    assert apply(out=attn.RowsStruct(0x1000, 128, 63)) == bad and apply(out=attn.RowsStruct(0x1000, 0, 64)) == bad
+    assert apply(scale=1e30) == bad and apply(cap=1e-30) == bad
     assert apply(ws=None) == bad and apply(ws=0x1010) == bad and apply(ws_bytes=8) == A.KNN_ERR_WORKSPACE_TOO_SMALL
 
     def tables(lengths=0x1000, news=0x1000, batch=2, table=0x1000, width=4, block=16, free=0x1000, n_free=3, starts=0x1000,
