@@ -71,9 +71,9 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     // The heads that share a K and V stand side by side: "rows" of the tile are rows and, within a row, its heads.
     const int group = p.hq / p.hkv, tiles = (int)(((int64_t)p.mask.n * group + kTileRows - 1) / kTileRows);
-    const int w = work_of(blockIdx.x, gridDim.x);
+    const Work work = work_of(blockIdx.x, p.hkv, tiles * p.splits);
     // the last rows first: with a causal mask they see the most keys
-    const int split = w % p.splits, tile = tiles - 1 - w / p.splits % tiles, kv = w / p.splits / tiles;
+    const int split = work.piece % p.splits, tile = tiles - 1 - work.piece / p.splits, kv = work.kv;
     const int line = tile * kTileRows + wave * 32 + (lane & 31), row = line / group, head = kv * group + line % group;
     __shared__ LocalDocs local;
     const Span see = keys_of_row(with_local(p.mask, local, tid), row);

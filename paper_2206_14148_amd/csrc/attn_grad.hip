@@ -57,8 +57,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     // (rows and, within a row, the heads that share a K and V, as in the forward pass)
     const int group = p.hq / p.hkv, tiles = (int)(((int64_t)p.mask.n * group + kTileRows - 1) / kTileRows);
-    const int w = work_of(blockIdx.x, gridDim.x);
-    const int tile = tiles - 1 - w % tiles, kv = w / tiles;
+    const Work work = work_of(blockIdx.x, p.hkv, tiles);
+    const int tile = tiles - 1 - work.piece, kv = work.kv;
     const int line = tile * kTileRows + wave * 32 + (lane & 31), row = line / group, head = kv * group + line % group;
     __shared__ LocalDocs local;
     const Span see = keys_of_row(with_local(p.mask, local, tid), row);
@@ -213,9 +213,9 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     __shared__ int ends[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const int tiles = (p.mask.m + kTileRows - 1) / kTileRows, group = p.hq / p.hkv;
-    const int w = work_of(blockIdx.x, gridDim.x);
+    const Work work = work_of(blockIdx.x, p.hkv, tiles * p.splits);
     // the first keys first: with a causal mask most rows see them
-    const int part = w % p.splits, tile = w / p.splits % tiles, kv = w / p.splits / tiles;
+    const int part = work.piece % p.splits, tile = work.piece / p.splits, kv = work.kv;
     const int key = tile * kTileRows + wave * 32 + (lane & 31);
     __shared__ LocalDocs local;
     const Span see = rows_of_key(with_local(p.mask, local, tid), key);
