@@ -67,7 +67,8 @@ typedef struct {
  * the keys; where that leaves compute units idle and the limit has room, the keys are cut into n_splits
  * ranges walked concurrently, whose unnormalised sums, maxima and totals (fp32) lie in the workspace until a
  * last kernel joins them in ascending range order.  The gradient keeps two fp32 numbers per row and head (the row
- * sums of dO * O, the log-sums), and for dK and dV cuts the rows of all heads that read them into n_splits parts likewise.
+ * sums of dO * O, the log-sums), and for dK and dV cuts the rows of all heads that read them into n_splits parts likewise,
+ * for dQ the keys into row_splits ranges.
  * Results differ between limits that give different n_splits by the rounding of those sums.
  */
 typedef struct {
@@ -75,7 +76,7 @@ typedef struct {
     int32_t hq, hkv, d;
     int32_t tile_rows;
     int32_t n_splits;
-    int32_t reserved;
+    int32_t row_splits; /* gradient: ranges of keys for dQ; 0 elsewhere */
     uint64_t workspace_bytes; /* <= limit */
     uint64_t min_limit_bytes; /* smallest limit that can run this shape */
 } attn_plan_t;

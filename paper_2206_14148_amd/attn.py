@@ -36,7 +36,7 @@ class OptionsStruct(ctypes.Structure):
 class AttnPlanStruct(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int64), ("m", ctypes.c_int64), ("hq", ctypes.c_int32), ("hkv", ctypes.c_int32),
                 ("d", ctypes.c_int32), ("tile_rows", ctypes.c_int32), ("n_splits", ctypes.c_int32),
-                ("reserved", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64),
+                ("row_splits", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64),
                 ("min_limit_bytes", ctypes.c_uint64)]
 
 
@@ -76,6 +76,7 @@ class AttnPlan:
     d: int
     tile_rows: int
     n_splits: int
+    row_splits: int
     workspace_bytes: int
     min_limit_bytes: int
 
@@ -311,7 +312,9 @@ class AttnCache:
     @staticmethod
     def empty(blocks: int, hkv: int, d: int, block: int, code: str = "int8", device="cuda") -> "AttnCache":
         """A cache of nothing yet; code "int8" or "e4m3"."""
-        dtype = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[code]
+        dtype = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}.get(code)
+        if dtype is None:
+            _refuse('code must be "int8" or "e4m3"')
         row = attn_cache_row(d)
         k = torch.zeros((blocks, hkv, block, row), dtype=torch.uint8, device=device).view(dtype)
         v = torch.zeros((blocks, hkv, row, block), dtype=torch.uint8, device=device).view(dtype)

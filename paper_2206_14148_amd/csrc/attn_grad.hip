@@ -57,8 +57,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     // (rows and, within a row, the heads that share a K and V, as in the forward pass)
     const int group = p.hq / p.hkv, tiles = (int)(((int64_t)p.mask.n * group + kTileRows - 1) / kTileRows);
-    const Work work = work_of(blockIdx.x, p.hkv, tiles);
-    const int tile = tiles - 1 - work.piece, kv = work.kv;
+    const Work work = work_of(blockIdx.x, p.hkv, tiles * p.row_splits);
+    const int split = work.piece % p.row_splits, tile = tiles - 1 - work.piece / p.row_splits, kv = work.kv;
     const int line = tile * kTileRows + wave * 32 + (lane & 31), row = line / group, head = kv * group + line % group;
     __shared__ LocalDocs local;
     const Span see = keys_of_row(with_local(p.mask, local, tid), row);
@@ -74,6 +74,12 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     __syncthreads();
     int first = __builtin_amdgcn_readfirstlane(ends[0]), last = __builtin_amdgcn_readfirstlane(ends[1]);
     if (first >= last) first = last = 0;
+    if (p.row_splits > 1) {  // this part's steps
+        const int64_t steps = (last - first + kTileKeys - 1) / kTileKeys;
+        const int s0 = (int)(steps * split / p.row_splits), s1 = (int)(steps * (split + 1) / p.row_splits);
+        last = min(last, first + s1 * kTileKeys);
+        first += s0 * kTileKeys;
+    }
 
     const int64_t at = (int64_t)head * p.mask.n + row;
     s16x8 q[kSteps], g[kSteps];
@@ -97,7 +103,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     }
     rowsum = sum_of_halves(rowsum);
     const float log_sum = see.inside ? p.lse[at] : 0.f, lse = log_sum == -kInf ? kInf : log_sum / p.scale;  // no keys: P = 0
-    if (see.inside && half == 0) {  // for the walk by keys, whose entries of Q and dO may stand in as zeros
+    if (see.inside && half == 0 && split == 0) {  // for the walk by keys, whose entries of Q and dO may stand in as zeros
         p.rowsums[at] = fabsf(rowsum) < kInf ? -lse : __builtin_nanf("");
         p.rowsums[(int64_t)p.hq * p.mask.n + at] = -rowsum;
     }
@@ -187,6 +193,14 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         done = entries == kFinite || all_finite();
     }
     if (!see.inside) return;
+    if (p.row_splits > 1) {
+        float* const parts = p.partial + (split * (int64_t)p.hq * p.mask.n + at) * p.d;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) put4(parts, 32 * b + 8 * a + 4 * half, p.d, sum[b] * p.scale, 4 * a);
+        return;
+    }
     unsigned short* const o = p.dq.data + row * p.dq.ld + head * p.dq.hs;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
@@ -397,6 +411,22 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
         }
 }
 
+// dQ of one row and head from the parts, in ascending order: a wave for each.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_grad_join_rows_kernel(Problem p) {
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = (int64_t)p.hq * p.mask.n, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= rows) return;
+    const int head = (int)(at / p.mask.n), row = (int)(at % p.mask.n);
+    if (!keys_of_row(p.mask, row).inside) return;
+    for (int c = lane; c < p.d; c += 64) {
+        float a = 0.f;
+#pragma unroll 8
+        for (int s = 0; s < p.row_splits; ++s) a += p.partial[(s * rows + at) * p.d + c];
+        p.dq.data[row * p.dq.ld + head * p.dq.hs + c] = (unsigned short)T::pack(a, 0.f);
+    }
+}
+
 // dK and dV of one key and head from the parts, in ascending order: a wave for each.
 template <typename T>
 __global__ __launch_bounds__(256) void attn_grad_join_kernel(Problem p) {
@@ -421,8 +451,12 @@ template <typename T, int DP>
 hipError_t launch_kernels(const Problem& p, hipStream_t stream) {
     const int64_t row_tiles = ((int64_t)p.mask.n * (p.hq / p.hkv) + kTileRows - 1) / kTileRows, key_tiles = (p.mask.m + kTileRows - 1) / kTileRows;
     const dim3 block(256);
-    if (row_tiles) attn_grad_rows_kernel<T, DP><<<dim3((unsigned)(row_tiles * p.hkv)), block, 0, stream>>>(p);
+    if (row_tiles) attn_grad_rows_kernel<T, DP><<<dim3((unsigned)(row_tiles * p.hkv * p.row_splits)), block, 0, stream>>>(p);
     hipError_t e = hipGetLastError();
+    if (e == hipSuccess && row_tiles && p.row_splits > 1) {
+        attn_grad_join_rows_kernel<T><<<dim3((unsigned)(((int64_t)p.mask.n * p.hq + 3) / 4)), block, 0, stream>>>(p);
+        e = hipGetLastError();
+    }
     if (e != hipSuccess || !key_tiles) return e;
     attn_grad_keys_kernel<T, DP><<<dim3((unsigned)(key_tiles * p.hkv * p.splits)), block, 0, stream>>>(p);
     e = hipGetLastError();

@@ -127,6 +127,25 @@ def test_work_split_along_the_keys_and_over_the_heads(dtype):
     check(*data, causal=True, limit=least)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_dq_from_ranges_of_the_keys(dtype):
+    for n, m, hq, hkv, d, o in [(1, 5000, 2, 1, 128, {}), (7, 4097, 4, 2, 64, {"causal": True, "cap": 20.0}),
+                                (140, 2100, 2, 2, 80, {"slopes": [0.01, 0.002], "causal": True}),
+                                (9, 1500, 2, 1, 33, {"starts": [1, 4, 9], "k_starts": [10, 400, 1490]})]:
+        plan = A.attn_grad_plan(n, m, hq, hkv, d, GB)
+        assert plan.row_splits > 1 and A.attn_grad_plan(n, m, hq, hkv, d, plan.min_limit_bytes).row_splits == 1
+        data = make(n, m, hq, hkv, d, dtype, m)
+        check(*data, **dict(o))
+        check(*data, limit=plan.min_limit_bytes, **dict(o))
+    # a key that is not finite makes the dQ of who sees it NaN, whichever range it lies in, and no other's
+    Q, K, V, dO = make(6, 3000, 2, 1, 64, dtype, 3)
+    assert A.attn_grad_plan(6, 3000, 2, 1, 64, GB).row_splits > 1
+    K[2995] = math.nan
+    O, lse = A.attn_apply(Q, K, V, GB, causal=True)
+    got = torch.isnan(A.attn_grad(Q, K, V, O, lse, dO, GB, causal=True)[0])
+    assert got[1:].all() and not got[0].any()
+
+
 def test_no_rows_and_no_keys():
     Q, K, V, dO = make(5, 4, 2, 1, 64, "bf16", 1)
     O, lse = A.attn_apply(Q[:0], K, V, GB)
