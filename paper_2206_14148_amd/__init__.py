@@ -1,8 +1,8 @@
-"""MI355X-native exact brute-force kNN and kernel matrix-vector product under a caller-given
+"""MI355X-native exact brute-force kNN, kernel matrix-vector product and attention under a caller-given
 device-memory limit.
 
-The package is a thin binding over libknn_mi355x.so (include/knn.h, include/kmv.h); see
-binding.py.
+The package is a thin binding over libknn_mi355x.so (include/knn.h, include/kmv.h, include/sgpr.h, include/attn.h); see
+binding.py and attn.py.
 """
 from .binding import (  # noqa: F401
     KNN_ERR_HIP, KNN_ERR_INVALID_ARG, KNN_ERR_MEM_LIMIT_TOO_SMALL, KNN_ERR_UNSUPPORTED,
