@@ -1,7 +1,6 @@
 // C ABI of the attention product, its gradient and its cache (see include/attn.h for the contract).
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <cstring>
 
 #include "../../include/attn.h"
@@ -151,13 +150,14 @@ extern "C" knn_status attn_grad_plan(int64_t n, int64_t m, int32_t hq, int32_t h
     const int64_t steps = (n + attn::kStepRows - 1) / attn::kStepRows * (hq / hkv);
     const int64_t shape[2] = {m * hkv, d};
     out->n_splits = m == 0 ? 1 : best_parts(tiles, steps, 0.5, 16.0 * m * hkv * d, mem_limit_bytes - sums, key_parts, shape);
-    // dQ likewise, whose parts are joined before dK and dV need the place (the gradient of 3 rows of 16 heads against 50021
+    const uint64_t of_keys = key_parts(shape, out->n_splits);
+    // dQ likewise, with the room that those leave (the gradient of 3 rows of 16 heads against 50021
     // keys: 1354 us without, 107 with 128 parts; 1000 rows against 4000 keys, 8 heads: 181 and 116)
     const int64_t row_tiles = (n * (hq / hkv) + attn::kTileRows - 1) / attn::kTileRows * hkv;
     const int64_t row_shape[2] = {n * hq, d};
     out->row_splits = n == 0 ? 1 : best_parts(row_tiles, (m + attn::kTileKeys - 1) / attn::kTileKeys, 1.0, 8.0 * n * hq * d,
-                                              mem_limit_bytes - sums, grad_row_parts, row_shape);
-    out->workspace_bytes = sums + std::max(key_parts(shape, out->n_splits), grad_row_parts(row_shape, out->row_splits));
+                                              mem_limit_bytes - sums - of_keys, grad_row_parts, row_shape);
+    out->workspace_bytes = sums + of_keys + grad_row_parts(row_shape, out->row_splits);
     return KNN_OK;
 }
 
@@ -224,6 +224,8 @@ extern "C" knn_status attn_grad(const attn_rows_t* Q, const attn_rows_t* K, cons
     p.row_splits = plan.row_splits;
     p.rowsums = static_cast<float*>(workspace);
     p.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + knn::align_up((uint64_t)n * hq * 8));
+    const int64_t keys_d[2] = {m * hkv, d};
+    p.row_partial = p.partial + key_parts(keys_d, p.splits) / 4;
     hipEvent_t t = knn::profile_mark(stream);
     const hipError_t e = attn::launch_grad(p, stream);
     if (e != hipSuccess) {

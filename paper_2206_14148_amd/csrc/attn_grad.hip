@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     }
     if (!see.inside) return;
     if (p.row_splits > 1) {
-        float* const parts = p.partial + (split * (int64_t)p.hq * p.mask.n + at) * p.d;
+        float* const parts = p.row_partial + (split * (int64_t)p.hq * p.mask.n + at) * p.d;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -411,10 +411,28 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
         }
 }
 
-// dQ of one row and head from the parts, in ascending order: a wave for each.
+// dQ of one row and head, or dK and dV of one key and head, from the parts, in ascending order: a wave for each.  One launch for
+// both, as it costs 5 us.
 template <typename T>
-__global__ __launch_bounds__(256) void attn_grad_join_rows_kernel(Problem p) {
+__global__ __launch_bounds__(256) void attn_grad_join_kernel(Problem p, int64_t row_blocks) {
     const int lane = threadIdx.x & 63;
+    if (blockIdx.x >= row_blocks) {
+        const int64_t keys = (int64_t)p.mask.m * p.hkv, at = ((int64_t)blockIdx.x - row_blocks) * 4 + (threadIdx.x >> 6);
+        if (at >= keys) return;
+        const int key = (int)(at / p.hkv), kv = (int)(at % p.hkv);
+        if (!rows_of_key(p.mask, key).inside) return;
+        for (int c = lane; c < p.d; c += 64) {
+            float a = 0.f, b = 0.f;
+            for (int s = 0; s < p.splits; ++s) {
+                const float* o = p.partial + (2 * s * keys + at) * p.d + c;
+                a += o[0];
+                b += o[keys * p.d];
+            }
+            p.dk.data[key * p.dk.ld + kv * p.dk.hs + c] = (unsigned short)T::pack(a, 0.f);
+            p.dv.data[key * p.dv.ld + kv * p.dv.hs + c] = (unsigned short)T::pack(b, 0.f);
+        }
+        return;
+    }
     const int64_t rows = (int64_t)p.hq * p.mask.n, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (at >= rows) return;
     const int head = (int)(at / p.mask.n), row = (int)(at % p.mask.n);
@@ -422,28 +440,8 @@ __global__ __launch_bounds__(256) void attn_grad_join_rows_kernel(Problem p) {
     for (int c = lane; c < p.d; c += 64) {
         float a = 0.f;
 #pragma unroll 8
-        for (int s = 0; s < p.row_splits; ++s) a += p.partial[(s * rows + at) * p.d + c];
+        for (int s = 0; s < p.row_splits; ++s) a += p.row_partial[(s * rows + at) * p.d + c];
         p.dq.data[row * p.dq.ld + head * p.dq.hs + c] = (unsigned short)T::pack(a, 0.f);
-    }
-}
-
-// dK and dV of one key and head from the parts, in ascending order: a wave for each.
-template <typename T>
-__global__ __launch_bounds__(256) void attn_grad_join_kernel(Problem p) {
-    const int lane = threadIdx.x & 63;
-    const int64_t keys = (int64_t)p.mask.m * p.hkv, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= keys) return;
-    const int key = (int)(at / p.hkv), kv = (int)(at % p.hkv);
-    if (!rows_of_key(p.mask, key).inside) return;
-    for (int c = lane; c < p.d; c += 64) {
-        float a = 0.f, b = 0.f;
-        for (int s = 0; s < p.splits; ++s) {
-            const float* o = p.partial + (2 * s * keys + at) * p.d + c;
-            a += o[0];
-            b += o[keys * p.d];
-        }
-        p.dk.data[key * p.dk.ld + kv * p.dk.hs + c] = (unsigned short)T::pack(a, 0.f);
-        p.dv.data[key * p.dv.ld + kv * p.dv.hs + c] = (unsigned short)T::pack(b, 0.f);
     }
 }
 
@@ -453,15 +451,12 @@ hipError_t launch_kernels(const Problem& p, hipStream_t stream) {
     const dim3 block(256);
     if (row_tiles) attn_grad_rows_kernel<T, DP><<<dim3((unsigned)(row_tiles * p.hkv * p.row_splits)), block, 0, stream>>>(p);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && row_tiles && p.row_splits > 1) {
-        attn_grad_join_rows_kernel<T><<<dim3((unsigned)(((int64_t)p.mask.n * p.hq + 3) / 4)), block, 0, stream>>>(p);
-        e = hipGetLastError();
-    }
-    if (e != hipSuccess || !key_tiles) return e;
-    attn_grad_keys_kernel<T, DP><<<dim3((unsigned)(key_tiles * p.hkv * p.splits)), block, 0, stream>>>(p);
+    if (e != hipSuccess) return e;
+    if (key_tiles) attn_grad_keys_kernel<T, DP><<<dim3((unsigned)(key_tiles * p.hkv * p.splits)), block, 0, stream>>>(p);
     e = hipGetLastError();
-    if (e != hipSuccess || p.splits == 1) return e;
-    attn_grad_join_kernel<T><<<dim3((unsigned)(((int64_t)p.mask.m * p.hkv + 3) / 4)), block, 0, stream>>>(p);
+    const int64_t row_blocks = p.row_splits > 1 ? ((int64_t)p.mask.n * p.hq + 3) / 4 : 0, key_blocks = p.splits > 1 ? ((int64_t)p.mask.m * p.hkv + 3) / 4 : 0;
+    if (e != hipSuccess || row_blocks + key_blocks == 0) return e;
+    attn_grad_join_kernel<T><<<dim3((unsigned)(row_blocks + key_blocks)), block, 0, stream>>>(p, row_blocks);
     return hipGetLastError();
 }
 

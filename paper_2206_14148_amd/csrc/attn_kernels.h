@@ -32,7 +32,8 @@ struct Problem {
     float* rowsums;  // gradient: [2][hq][n], what a row takes off its products: -log-sum / scale, -sum of dO * O
     float* partial;  // n_splits > 1
     int splits;
-    int row_splits;  // gradient: parts of dQ, which lie in `partial` before those of dK and dV do
+    int row_splits;      // gradient: parts of dQ,
+    float* row_partial;  // row_splits > 1: [row_splits][hq][n][d]
 };
 
 hipError_t launch_forward(const Problem& p, hipStream_t stream);

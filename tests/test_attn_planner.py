@@ -42,7 +42,7 @@ def test_plans_stay_under_their_limit_and_count_what_they_keep(n, m, hq, hkv, d)
         g = A.attn_grad_plan(n, m, hq, hkv, d, limit)
         assert g.min_limit_bytes == least and 1 <= g.n_splits <= 256
         parts = [up(s * size * d * 4) if s > 1 else 0 for s, size in ((g.n_splits, 2 * m * hkv), (g.row_splits, n * hq))]
-        assert g.workspace_bytes == least + max(parts) <= limit and 1 <= g.row_splits <= 256
+        assert g.workspace_bytes == least + sum(parts) <= limit and 1 <= g.row_splits <= 256
 
 
 def test_shapes_that_are_refused():
