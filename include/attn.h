@@ -120,7 +120,9 @@ knn_status attn_apply(const attn_rows_t *Q, const attn_rows_t *K, const attn_row
  *   workspace_bytes >= attn_grad_plan(...).workspace_bytes
  * Rows and keys outside the documents are left as they were.  P and ds are rounded to the type of Q for
  * the products, whose sums are fp32 in a fixed order: no atomics, the same bits on every call.
- * An entry that is not finite makes the gradients not finite of the rows and keys that it meets, and no others.
+ * Entries that are not finite.  One in a row's Q or dO (or O) makes its dQ, and dK and dV of the keys that it sees, not finite, one in K
+ * the dQ of the rows that see it, and so on by the formulas where a score is NaN or +infinity (the row's log-sum is NaN); no others.
+ * A row that sees no key, or whose scores are all -infinity, has dQ = 0 and adds nothing to the others.
  * How exact: P is made from lse, which holds a score to 2^-24 of itself; <dO, O> takes the O that attn_apply rounded, so
  * where one key has nearly all of a row's weight its ds, a small difference, is off by that rounding.
  */

@@ -48,6 +48,25 @@ struct Scores {
     }
 };
 
+// Which of a tile's 64 rows hold an entry that is not finite: a bit for each, the same in all lanes.
+template <typename T, typename L>
+__device__ __forceinline__ uint64_t not_finite(const unsigned char* lds, int lane) {
+    constexpr unsigned kExp = T::kExponents & 0xffffu;
+    bool bad = false;
+#pragma unroll 1
+    for (int piece = 0; piece < L::kPieces; ++piece) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(lds + lane * L::kRowBytes + 16 * piece);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad = bad || (w[e] & kExp) == kExp || (w[e] >> 16 & kExp) == kExp;
+    }
+    return __ballot(bad);
+}
+// Bits low .. high - 1 of 64.
+__device__ __forceinline__ uint64_t bits_between(int low, int high) {
+    auto below = [](int x) { return x <= 0 ? (uint64_t)0 : x >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << x) - 1; };
+    return below(high) & ~below(low);
+}
+
 template <typename T, int DP>
 __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     typedef Tile<DP> L;
@@ -83,7 +102,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
 
     const int64_t at = (int64_t)head * p.mask.n + row;
     s16x8 q[kSteps], g[kSteps];
-    float rowsum = 0.f;
+    float rowsum = 0.f, zero = 0.f;  // zero: NaN if an entry of Q is not finite
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
         u32x4 a = {0, 0, 0, 0}, b = a, c = a;
@@ -99,13 +118,19 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         for (int e = 0; e < 4; ++e) {
             rowsum = __builtin_fmaf(T::low(b[e]), T::low(c[e]), rowsum);
             rowsum = __builtin_fmaf(T::high(b[e]), T::high(c[e]), rowsum);
+            zero = __builtin_fmaf(T::low(a[e]), 0.f, __builtin_fmaf(T::high(a[e]), 0.f, zero));
         }
     }
     rowsum = sum_of_halves(rowsum);
-    const float log_sum = see.inside ? p.lse[at] : 0.f, lse = log_sum == -kInf ? kInf : log_sum / p.scale;  // no keys: P = 0
+    const float log_sum = see.inside ? p.lse[at] : 0.f;
+    const bool none = log_sum == -kInf;  // no keys: P = 0
+    const float lse = none ? kInf : log_sum / p.scale;
+    // An entry of Q, dO or O that is not finite (those of dO and O reach the row sum): the row's gradients and those of the keys
+    // that it sees are NaN, whatever its scores come to (an infinity behind a cap gives finite ones).
+    bool lost = sum_of_halves(zero) != 0.f || !(fabsf(rowsum) < kInf);
     if (see.inside && half == 0 && split == 0) {  // for the walk by keys, whose entries of Q and dO may stand in as zeros
-        p.rowsums[at] = fabsf(rowsum) < kInf ? -lse : __builtin_nanf("");
-        p.rowsums[(int64_t)p.hq * p.mask.n + at] = -rowsum;
+        p.rowsums[at] = none || !lost ? -lse : __builtin_nanf("");
+        p.rowsums[(int64_t)p.hq * p.mask.n + at] = none ? 0.f : -rowsum;
     }
     Scores to(p);
     if (see.inside) to.of_head(p, head);
@@ -117,8 +142,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     auto begin = [&]() {
         for (int b = 0; b < kBlocks; ++b) sum[b] = f32x16{};
     };
-    // One tile that lies in LDS.
-    auto tile_of = [&](int j0) {
+    // One tile that lies in LDS, its rows as the last product takes them at `last_keys`.
+    auto tile_of = [&](int j0, const unsigned char* last_keys) {
         if (j0 >= high || j0 + kTileKeys <= low) return;
         const bool edge = j0 < all_low || j0 + kTileKeys > all_high;
 #pragma unroll
@@ -144,8 +169,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
             const s16x8 w0 = rounded_operand<T>(y, 0), w1 = rounded_operand<T>(y, 1);
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
-                sum[b] = T::mfma(at_lane.column(keys, b, 2 * t), w0, sum[b]);
-                sum[b] = T::mfma(at_lane.column(keys, b, 2 * t + 1), w1, sum[b]);
+                sum[b] = T::mfma(at_lane.column(last_keys, b, 2 * t), w0, sum[b]);
+                sum[b] = T::mfma(at_lane.column(last_keys, b, 2 * t + 1), w1, sum[b]);
             }
             __builtin_amdgcn_sched_barrier(0);  // (the halves do not mix: registers)
         }
@@ -172,33 +197,41 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         for (int j0 = first; j0 < last; j0 += kTileKeys, buffer ^= L::kBytes, at_lane.other(L::kBytes)) {
             arrive_and_wait();
             if (j0 + kTileKeys < last) bring(j0 + kTileKeys, buffer ^ L::kBytes);
-            tile_of(j0);
+            tile_of(j0, keys);
         }
         done = all_finite();
         at_lane = Lane<DP>(lane);
         entries = kFinite;
     }
     // Without 16-byte reads; and where a sum came out not finite.  An entry of K that is not finite meets the zero weights
-    // of rows that do not see it as well.  Then the workgroup walks once more with those entries as zeros: the rows that
-    // see one have a log-sum that is NaN, and with it P.
+    // of rows that do not see it as well.  Then the workgroup walks once more, with zeros in the place of those entries
+    // for the product with ds alone (the scores are made of what K holds), and keeps in mind which rows see one: of
+    // those, and of no others, the gradient is NaN, as 0 * infinity is.
     for (; !done; ++entries) {
         begin();
         for (int j0 = first; j0 < last; j0 += kTileKeys) {
             arrive_and_wait();
-            stage<T, DP, 256>(keys, p.k, kv, j0, first, last, p.d, tid, entries);
+            stage<T, DP, 256>(keys, p.k, kv, j0, first, last, p.d, tid, kAsTheyAre);
             stage<T, DP, 256>(values, p.v, kv, j0, first, last, p.d, tid, kAsTheyAre);
+            if (entries == kFinite) stage<T, DP, 256>(keys + L::kBytes, p.k, kv, j0, first, last, p.d, tid, kFinite);
             arrive_and_wait();
-            tile_of(j0);
+            if (entries == kFinite) {
+                const uint64_t bad = not_finite<T, L>(keys, lane);
+                lost = lost || (bad & bits_between(see.lo - j0, see.hi - j0));
+            }
+            tile_of(j0, entries == kFinite ? keys + L::kBytes : keys);
         }
         done = entries == kFinite || all_finite();
     }
     if (!see.inside) return;
+    const float times = none ? 0.f : lost ? __builtin_nanf("") : p.scale;
+    if (none) begin();
     if (p.row_splits > 1) {
         float* const parts = p.row_partial + (split * (int64_t)p.hq * p.mask.n + at) * p.d;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int a = 0; a < 4; ++a) put4(parts, 32 * b + 8 * a + 4 * half, p.d, sum[b] * p.scale, 4 * a);
+            for (int a = 0; a < 4; ++a) put4(parts, 32 * b + 8 * a + 4 * half, p.d, sum[b] * times, 4 * a);
         return;
     }
     unsigned short* const o = p.dq.data + row * p.dq.ld + head * p.dq.hs;
@@ -208,7 +241,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         for (int a = 0; a < 4; ++a) {
             float x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = sum[b][4 * a + e] * p.scale;
+            for (int e = 0; e < 4; ++e) x[e] = sum[b][4 * a + e] * times;
             put4<T>(o, 32 * b + 8 * a + 4 * half, p.d, p.dq.wide, x);
         }
 }
@@ -360,8 +393,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
         at_lane = Lane<DP>(lane);
         entries = kFinite;
     }
-    // As by rows: entries of Q and dO that are not finite as zeros in a second walk.  Their rows have a log-sum or a
-    // row sum, and with it P, that is NaN.
+    // Entries of Q and dO that are not finite as zeros in a second walk.  Their rows have a log-sum that the walk by rows
+    // has made NaN, and with it P (or minus infinity, and P = 0).
     for (; !done; ++entries) {
         begin();
         for (int head = head0; head < head1; ++head) {

@@ -1,0 +1,110 @@
+"""Attention over the range of what it accepts: entries that are not finite, on each way of reading rows and with the work in parts.  Values and bounds: attn_bounds.py."""
+import pytest
+
+import paper_2206_14148_amd as A
+
+torch = pytest.importorskip("torch")
+from attn_bounds import attention, compare  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+GB = 10 ** 9
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16}
+INF = float("inf")
+NAMES = ("O", "lse", "dQ", "dK", "dV")
+
+
+def make(n, m, hq, hkv, d, dtype, seed, sizes=(1.0, 1.0, 1.0, 1.0)):
+    gen = torch.Generator().manual_seed(seed)
+    shapes = ((n, hq), (m, hkv), (m, hkv), (n, hq))
+    return [(torch.randn(r, h, d, generator=gen) * s).to(TYPES[dtype]).cuda() for (r, h), s in zip(shapes, sizes)]
+
+
+def words(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def odd(t):
+    """The same rows where they cannot be read 16 bytes at a time."""
+    view = torch.zeros(t.shape[0], t.shape[1], t.shape[2] + 3, dtype=t.dtype, device="cuda")[:, :, 1:1 + t.shape[2]]
+    view.copy_(t)
+    return view
+
+
+def check(Q, K, V, dO, limit=GB, names=NAMES, **o):
+    device = {k: words(v) if k in ("starts", "k_starts", "prefix") else torch.tensor(v, device="cuda") if k == "slopes" else v
+              for k, v in o.items()}
+    O, lse = A.attn_apply(Q, K, V, limit, **device)
+    got = (O, lse) + (tuple(A.attn_grad(Q, K, V, O, lse, dO, limit, **device)) if names == NAMES else ())
+    torch.cuda.synchronize()
+    r = attention(Q, K, V, dO if names == NAMES else None, **o)
+    return got, r, [compare(name, t, r) for name, t in zip(names, got)]
+
+
+# ---- entries that are not finite ------------------------------------------------------------
+
+@pytest.mark.parametrize("reading", ["16 bytes", "entries"])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 96)])
+def test_infinities_reach_the_gradients_of_who_meets_them(dtype, d, cap, reading):
+    """An infinity in Q, K, V or dO, of either sign: not finite where it is met, whatever the scores come to, and
+    nothing changed for the others."""
+    starts = [0, 90, 200]
+    o = dict(causal=True, cap=cap, starts=starts)
+    clean = make(200, 200, 4, 2, d, dtype, 4)
+    clean[0][60:90, :, 0] = clean[0][60:90, :, 0].abs() + 0.5  # one sign: K = -infinity hides that key from all of them
+    moved = odd if reading == "entries" else lambda t: t
+    clean = [moved(t) for t in clean]
+    first, _, _ = check(*clean, **o)
+    for which, row, head in ((0, 100, 1), (1, 60, 1), (2, 150, 0), (3, 30, 2)):
+        for value in (INF, -INF, float("nan")):
+            data = [t.clone() if reading == "16 bytes" else odd(t) for t in clean]
+            data[which][row, head, 0] = value
+            got, r, _ = check(*data, **o)
+            # whoever does not meet it has the same bits
+            document = (0, 90) if row < 90 else (90, 200)
+            heads = range(4) if which in (0, 3) else (2 * head, 2 * head + 1)
+            heads = [head] if which in (0, 3) else list(heads)
+            kv = heads[0] // 2
+            q_met, k_met = torch.zeros(200, 4, dtype=torch.bool), torch.zeros(200, 2, dtype=torch.bool)
+            for h in heads:
+                q_met[(row if which in (0, 3) else row):(row + 1 if which in (0, 3) else document[1]), h] = True
+            k_met[document[0]:document[1], kv] = True
+            for name, a, b, met in zip(NAMES, got, first, (q_met, q_met.T, q_met, k_met, k_met)):
+                same = (a == b) | (torch.isnan(a) & torch.isnan(b))
+                same = same.cpu() if name == "lse" else same.all(2).cpu()
+                assert (same | met).all(), (which, value, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_infinities_where_the_work_is_in_parts(dtype, cap):
+    n, m, d = 6, 3000, 64
+    plan, grad = A.attn_plan(n, m, 2, 1, d, GB), A.attn_grad_plan(n, m, 2, 1, d, GB)
+    assert plan.n_splits > 1 and grad.row_splits > 1
+    for which, row in ((1, 2997), (1, 40), (2, 2998), (2, 1500), (0, 3), (3, 2)):
+        for value in (INF, -INF):
+            data = make(n, m, 2, 1, d, dtype, 5)
+            data[0][:, :, 1] = data[0][:, :, 1].abs() + 0.25
+            data[which][row, 0, 1] = value
+            check(*data, causal=True, cap=cap)
+    # the gradient by keys in parts: many rows, few keys
+    assert A.attn_grad_plan(700, 130, 2, 1, d, GB).n_splits > 1
+    for which, row in ((0, 600), (3, 17), (1, 100)):
+        data = make(700, 130, 2, 1, d, dtype, 6)
+        data[which][row, 0, 1] = -INF
+        check(*data, cap=cap)
+
+
+def test_rows_whose_scores_are_all_minus_infinity():
+    """They count as rows that see no key, with an infinity of their own as well."""
+    for which in (0, 1):
+        data = make(70, 50, 2, 1, 64, "bf16", 8)
+        data[0][:, :, 0] = data[0][:, :, 0].abs() + 0.5
+        data[1][:, :, 0] = -data[1][:, :, 0].abs() - 0.5
+        if which:
+            data[1][:, 0, 0] = -INF
+        else:
+            data[0][33, 1, 0] = INF
+        got, r, _ = check(*data)
+        lost = r["lse"] == -INF
+        assert lost.any() and (got[2].cpu()[lost.T] == 0).all() and (got[0].cpu()[lost.T] == 0).all()
