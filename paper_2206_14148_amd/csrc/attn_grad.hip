@@ -31,7 +31,7 @@ struct Scores {
         if (capped) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * (x[e] + lse(e)))), 1.f);
+                const float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * x[e])), 1.f);
                 y[e] *= __builtin_fmaf(-t, t, 1.f);
                 x[e] = __builtin_fmaf(from_cap, t, -lse(e));
             }
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             f32x16 x, y;
-            float x_less = -lse, y_less = -rowsum;
+            float x_less = to.capped ? 0.f : -lse, y_less = -rowsum;
             asm("" : "+v"(x_less), "+v"(y_less));  // (or 32 registers hold them sixteen times all along)
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] = x_less, y[e] = y_less;
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
         f32x16 x, y;
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-            const f32x4 lse = *reinterpret_cast<const f32x4*>(&of_rows[buffer][0][8 * a + 4 * half]);
+            const f32x4 lse = to.capped ? f32x4{} : *reinterpret_cast<const f32x4*>(&of_rows[buffer][0][8 * a + 4 * half]);
             const f32x4 rowsum = *reinterpret_cast<const f32x4*>(&of_rows[buffer][1][8 * a + 4 * half]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
