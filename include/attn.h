@@ -54,7 +54,7 @@ typedef struct {
     int32_t dtype;            /* attn_dtype */
     int32_t causal;           /* 0 or 1 */
     double scale;             /* 2^-60 .. 2^60 */
-    double cap;               /* 0: none; else 2^-60 .. 2^60 */
+    double cap;               /* 0: none; else 2^-60 .. 2^60.  Scores are off by 2^-23 of a cap up to 64, beyond by steps of 2^-24 of themselves */
     const float *slopes;      /* DEVICE [hq], finite; NULL: none.  Not differentiated */
     int64_t docs;             /* >= 1 with starts; without starts there is one document */
     const int32_t *starts;    /* DEVICE [docs + 1], ascending, within 0 .. n; NULL: 0, n */

@@ -438,7 +438,7 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheProblem p) {
             q[s][k] = __builtin_bit_cast(s16x8, v);
         }
     }
-    const float to_cap = p.cap > 0.f ? 2.f * kLog2e * p.scale / p.cap : 0.f, from_cap = p.cap * kLog2e;
+    const float to_cap = p.cap > 0.f ? (p.cap > kLargeCap ? 1.f : 2.f * kLog2e) * p.scale / p.cap : 0.f, from_cap = p.cap * kLog2e;
     const int seen_by_all = length - p.nq + 1;  // tokens below this are seen by every row
 
     f32x4 sum[SETS][kTiles];
@@ -497,7 +497,12 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheProblem p) {
                     x[t] = codes_mfma<T, E4M3>(u32x2{kc[t][k / 2][2 * (k % 2)], kc[t][k / 2][2 * (k % 2) + 1]}, q[s][k], x[t]);
             }
             const float factor = p.scale * kLog2e * ks;
-            if (p.cap > 0.f) {
+            if (p.cap > kLargeCap) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[t][e] = from_cap * tanh_of(to_cap * ks * x[t][e]);
+            } else if (p.cap > 0.f) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll

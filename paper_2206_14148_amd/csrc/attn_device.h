@@ -69,6 +69,23 @@ struct F16 {
     static __device__ __forceinline__ float high(unsigned w) { return (float)__builtin_bit_cast(v2, w)[1]; }
 };
 
+// Caps.  1 - 2 / (1 + exp(2 z)) is off by some 2^-23 however small its tanh(z) is, so a score by 2^-23 of the cap: up to kLargeCap
+// that is less than 1e-5.  Beyond it a z below 1/2 has its series instead, which is off by steps of 2^-24 of the score itself
+// (tanh z = z - z^3 / 3 + 2 z^5 / 15 - ...; what is left out behind z^15 is below 2^-26 of it).  Both are made for every
+// score, twelve instructions more.  8000 rows, 16 heads, d = 64, f16: 210 us without a cap, 316 with 50, 488 with 65; gradient of
+// 4096 rows, 32 heads on 8, d = 128, bf16, causal: 542, 652, 756; the cache's 200003 tokens, 32 heads on 8: 88, 87, 88.
+constexpr float kLargeCap = 64.f;
+__device__ __forceinline__ float tanh_of(float z) {
+    constexpr float c[] = {1.f, -1.f / 3.f, 2.f / 15.f, -17.f / 315.f, 62.f / 2835.f, -1382.f / 155925.f, 21844.f / 6081075.f,
+                           -929569.f / 638512875.f};
+    const float w = z * z;
+    float series = c[7];
+#pragma unroll
+    for (int i = 6; i >= 0; --i) series = __builtin_fmaf(series, w, c[i]);
+    const float far = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * kLog2e * z)), 1.f);
+    return fabsf(z) < 0.5f ? z * series : far;
+}
+
 // what lane ^ 32 holds, combined with one's own
 __device__ __forceinline__ u32x2 both_halves(float v) {
     return __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);

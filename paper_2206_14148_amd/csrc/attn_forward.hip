@@ -62,7 +62,7 @@ __device__ __forceinline__ void write_rows(const Problem& p, const Span& see, in
 // unit (a maximum, a product, an exponential, a sum and half a conversion for each score) for about as much, and
 // the clock falls to 1.8 GHz: an order of instructions that kept the matrix cores 14 % busier took the same time.
 // With a cap another exponential and a reciprocal come to each score, and the vector unit alone bounds it.
-template <typename T, int DP>
+template <typename T, int DP, bool LARGE_CAP>  // cap > kLargeCap
 __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     typedef Tile<DP> L;
     constexpr int kBlocks = DP / 32, kSteps = DP / 16;
@@ -102,8 +102,8 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     }
     // What the walk calls a score is u / scale: the product itself, and a cap and slopes divided by the scale.
     const float factor = p.scale * kLog2e;  // of a score, to powers of two
-    const bool capped = p.cap > 0.f;
-    const float to_cap = capped ? 2.f * factor / p.cap : 0.f, from_cap = p.cap / p.scale;
+    const bool capped = LARGE_CAP || p.cap > 0.f;
+    const float to_cap = LARGE_CAP ? p.scale / p.cap : capped ? 2.f * factor / p.cap : 0.f, from_cap = p.cap / p.scale;
     const float slope = p.slopes && see.inside ? p.slopes[head] / p.scale : 0.f;
     const float slack = kSlack / factor;
 
@@ -130,7 +130,12 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     };
     // A tile's products x to what the weights are the exponentials of.
     auto scores = [&](f32x16* x, int j0) {
-        if (capped) {
+        if (LARGE_CAP) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[t][e] = __builtin_fmaf(from_cap, tanh_of(to_cap * x[t][e]), -top);
+        } else if (capped) {
             const float one = from_cap - top, two = -2.f * from_cap;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -270,16 +275,25 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Problem p) {
     if (p.lse && lane == 0) p.lse[at] = r.total == 0.f ? -kInf : (r.top + __builtin_amdgcn_logf(r.total)) * kLn2;
 }
 
+template <typename T, bool LARGE_CAP>
+void launch_walk(const Problem& p, dim3 grid, hipStream_t stream) {
+    if (p.d <= 64)
+        attn_forward_kernel<T, 64, LARGE_CAP><<<grid, dim3(256), 0, stream>>>(p);
+    else if (p.d <= 96)
+        attn_forward_kernel<T, 96, LARGE_CAP><<<grid, dim3(256), 0, stream>>>(p);
+    else
+        attn_forward_kernel<T, 128, LARGE_CAP><<<grid, dim3(256), 0, stream>>>(p);
+}
+
 template <typename T>
 hipError_t launch(const Problem& p, hipStream_t stream) {
     const int64_t tiles = ((int64_t)p.mask.n * (p.hq / p.hkv) + kTileRows - 1) / kTileRows;
     const dim3 grid((unsigned)(tiles * p.hkv * p.splits)), block(256);
-    if (p.d <= 64)
-        attn_forward_kernel<T, 64><<<grid, block, 0, stream>>>(p);
-    else if (p.d <= 96)
-        attn_forward_kernel<T, 96><<<grid, block, 0, stream>>>(p);
+    // (a kernel of its own: as a branch the series of large caps cost the walks without it 2 %)
+    if (p.cap > kLargeCap)
+        launch_walk<T, true>(p, grid, stream);
     else
-        attn_forward_kernel<T, 128><<<grid, block, 0, stream>>>(p);
+        launch_walk<T, false>(p, grid, stream);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t rows = (int64_t)p.hq * p.mask.n;

@@ -11,16 +11,17 @@ namespace {
 // 16 products x = <Q, K>, less lse / scale, and y = <dO, V>, less the row sum, to P and P y (1 - tanh^2).  Both come with what
 // is taken off as their products' first summand; with a cap x comes without.  Scores are in units of the product: a cap, slopes and
 // the log-sum are divided by the scale.  `lse` gives number e's log-sum and `far` how far its row stands from its key.
+template <bool LARGE_CAP>  // cap > kLargeCap
 struct Scores {
     float factor, to_cap, from_cap, slope, per_scale;
     bool capped, sloped;
     __device__ __forceinline__ explicit Scores(const Problem& p) {
-        capped = p.cap > 0.f;
+        capped = LARGE_CAP || p.cap > 0.f;
         sloped = p.slopes;
         slope = 0.f;
         per_scale = 1.f / p.scale;
         factor = p.scale * kLog2e;
-        to_cap = capped ? 2.f * factor / p.cap : 0.f;
+        to_cap = LARGE_CAP ? p.scale / p.cap : capped ? 2.f * factor / p.cap : 0.f;
         from_cap = p.cap / p.scale;
     }
     __device__ __forceinline__ void of_head(const Problem& p, int head) {
@@ -31,7 +32,8 @@ struct Scores {
         if (capped) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * x[e])), 1.f);
+                const float t = LARGE_CAP ? tanh_of(to_cap * x[e])
+                                          : __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(to_cap * x[e])), 1.f);
                 y[e] *= __builtin_fmaf(-t, t, 1.f);
                 x[e] = __builtin_fmaf(from_cap, t, -lse(e));
             }
@@ -67,7 +69,7 @@ __device__ __forceinline__ uint64_t bits_between(int low, int high) {
     return below(high) & ~below(low);
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool LARGE_CAP>
 __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     typedef Tile<DP> L;
     constexpr int kBlocks = DP / 32, kSteps = DP / 16;
@@ -132,7 +134,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         p.rowsums[at] = none || !lost ? -lse : __builtin_nanf("");
         p.rowsums[(int64_t)p.hq * p.mask.n + at] = none ? 0.f : -rowsum;
     }
-    Scores to(p);
+    Scores<LARGE_CAP> to(p);
     if (see.inside) to.of_head(p, head);
 
     f32x16 sum[kBlocks];
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
 // or 800 TFLOP/s of its four products (with V in registers and 64 rows a step one workgroup, and 444 us); the walk by rows
 // takes 245 us for its three, 840 TFLOP/s.  What bounds both is the matrix cores' share: the vector instructions of the
 // exponentials (some 10 for a score) take nearly as long as the products, and hide behind the other workgroup's only in part.
-template <typename T, int DP>
+template <typename T, int DP, bool LARGE_CAP>
 __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     typedef Tile<DP, kStepRows> L;
     constexpr int kBlocks = DP / 32, kSteps = DP / 16;
@@ -313,7 +315,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     const int from_key = see.at - key + 4 * half, from_first = 4 * half - see.lo;
     const unsigned seen = see.hi - see.lo;
     // 32 rows that lie in LDS.
-    Scores to(p);
+    Scores<LARGE_CAP> to(p);
     auto tile_of = [&](int i0, int buffer) {
         if (i0 >= high || i0 + kStepRows <= low) return;
         const unsigned own = at_lane.rows ^ (buffer ? L::kBytes : 0);
@@ -478,14 +480,14 @@ __global__ __launch_bounds__(256) void attn_grad_join_kernel(Problem p, int64_t 
     }
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool LARGE_CAP>
 hipError_t launch_kernels(const Problem& p, hipStream_t stream) {
     const int64_t row_tiles = ((int64_t)p.mask.n * (p.hq / p.hkv) + kTileRows - 1) / kTileRows, key_tiles = (p.mask.m + kTileRows - 1) / kTileRows;
     const dim3 block(256);
-    if (row_tiles) attn_grad_rows_kernel<T, DP><<<dim3((unsigned)(row_tiles * p.hkv * p.row_splits)), block, 0, stream>>>(p);
+    if (row_tiles) attn_grad_rows_kernel<T, DP, LARGE_CAP><<<dim3((unsigned)(row_tiles * p.hkv * p.row_splits)), block, 0, stream>>>(p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (key_tiles) attn_grad_keys_kernel<T, DP><<<dim3((unsigned)(key_tiles * p.hkv * p.splits)), block, 0, stream>>>(p);
+    if (key_tiles) attn_grad_keys_kernel<T, DP, LARGE_CAP><<<dim3((unsigned)(key_tiles * p.hkv * p.splits)), block, 0, stream>>>(p);
     e = hipGetLastError();
     const int64_t row_blocks = p.row_splits > 1 ? ((int64_t)p.mask.n * p.hq + 3) / 4 : 0, key_blocks = p.splits > 1 ? ((int64_t)p.mask.m * p.hkv + 3) / 4 : 0;
     if (e != hipSuccess || row_blocks + key_blocks == 0) return e;
@@ -493,9 +495,15 @@ hipError_t launch_kernels(const Problem& p, hipStream_t stream) {
     return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, bool LARGE_CAP>
 hipError_t launch(const Problem& p, hipStream_t stream) {
-    return p.d <= 64 ? launch_kernels<T, 64>(p, stream) : p.d <= 96 ? launch_kernels<T, 96>(p, stream) : launch_kernels<T, 128>(p, stream);
+    return p.d <= 64   ? launch_kernels<T, 64, LARGE_CAP>(p, stream)
+           : p.d <= 96 ? launch_kernels<T, 96, LARGE_CAP>(p, stream)
+                       : launch_kernels<T, 128, LARGE_CAP>(p, stream);
+}
+template <typename T>
+hipError_t launch(const Problem& p, hipStream_t stream) {  // (both forms in one kernel would not fit its registers)
+    return p.cap > kLargeCap ? launch<T, true>(p, stream) : launch<T, false>(p, stream);
 }
 
 }  // namespace

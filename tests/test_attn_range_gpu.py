@@ -1,10 +1,11 @@
-"""Attention over the range of what it accepts: entries that are not finite, on each way of reading rows and with the work in parts.  Values and bounds: attn_bounds.py."""
+"""Attention over the whole range of what it accepts: entries that are not finite, caps of every size, on each way of reading rows and with the work in parts.  Values and bounds: attn_bounds.py."""
 import pytest
 
 import paper_2206_14148_amd as A
 
 torch = pytest.importorskip("torch")
-from attn_bounds import attention, compare  # noqa: E402
+import attn_formulas as F  # noqa: E402
+from attn_bounds import STEP32, attention, compare  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 GB = 10 ** 9
@@ -43,7 +44,7 @@ def check(Q, K, V, dO, limit=GB, names=NAMES, **o):
 # ---- entries that are not finite ------------------------------------------------------------
 
 @pytest.mark.parametrize("reading", ["16 bytes", "entries"])
-@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("cap", [0.0, 20.0, 1e5])
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 96)])
 def test_infinities_reach_the_gradients_of_who_meets_them(dtype, d, cap, reading):
     """An infinity in Q, K, V or dO, of either sign: not finite where it is met, whatever the scores come to, and
@@ -108,3 +109,38 @@ def test_rows_whose_scores_are_all_minus_infinity():
         got, r, _ = check(*data)
         lost = r["lse"] == -INF
         assert lost.any() and (got[2].cpu()[lost.T] == 0).all() and (got[0].cpu()[lost.T] == 0).all()
+
+
+# ---- caps -----------------------------------------------------------------------------------
+
+CAPS = [0.5, 64.0, 65.0, 300.0, 1e4, 1e6, 1e9, 2.0 ** 60]
+
+
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("cap", CAPS)
+def test_caps_of_every_size(cap, dtype):
+    for d, size in ((64, 1.0), (128, 3.0), (80, 40.0)):
+        check(*make(150, 211, 4, 2, d, dtype, 7, (size, 1.0, 1.0, 1.0)), cap=cap, causal=d == 128)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("cap", CAPS)
+def test_caps_of_every_size_over_the_cache(cap, code):
+    d, hq, hkv, block, lengths = 64, 4, 2, 16, [5, 130, 700]
+    gen = torch.Generator().manual_seed(3)
+    cache = A.AttnCache.empty(60, hkv, d, block, code)
+    K, V = (torch.randn(sum(lengths), hkv, d, generator=gen).half().cuda() for _ in range(2))
+    table = torch.zeros(3, 44, dtype=torch.int32, device="cuda")
+    slots = A.attn_cache_map(words(lengths), words(lengths), table, torch.arange(60, dtype=torch.int32, device="cuda"), block,
+                             sum(lengths))[2]
+    A.attn_cache_append(cache, K, V, slots)
+    Q = (6 * torch.randn(3, 2, hq, d, generator=gen)).half().cuda()
+    got = A.attn_cache_apply(Q, cache, table, words(lengths), GB, cap=cap).double().cpu()
+    k, v = cache.k.cpu().float().double(), cache.v.cpu().float().double()
+    scales = cache.k_scale.cpu(), cache.v_scale.cpu()
+    O, most = F.cache_attention(Q, k, v, *scales, table.tolist(), lengths, d, block, cap=cap)
+    if cap > 64:  # the bound without a cap, whose scores these are or smaller ones; 16 steps more of a score
+        _, most = F.cache_attention(Q, k, v, *scales, table.tolist(), lengths, d, block)
+        score = d ** -0.5 * float(Q.abs().double().sum(3).max()) * float((k.abs().amax((2, 3)) * scales[0]).max())
+        most = most + 4 * 16 * STEP32 * score * float((v.abs().amax((2, 3)) * scales[1]).max())
+    assert ((got - O).abs() <= most).all(), ((got - O).abs() / most).max()
