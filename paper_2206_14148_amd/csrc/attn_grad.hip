@@ -11,7 +11,7 @@ namespace {
 // 16 products x = <Q, K>, less lse / scale, and y = <dO, V>, less the row sum, to P and P y (1 - tanh^2).  Both come with what
 // is taken off as their products' first summand; with a cap x comes without.  Scores are in units of the product: a cap, slopes and
 // the log-sum are divided by the scale.  `lse` gives number e's log-sum and `far` how far its row stands from its key.
-template <bool LARGE_CAP>  // cap > kLargeCap
+template <bool LARGE_CAP, bool POWERS>  // cap > kLargeCap
 struct Scores {
     float factor, to_cap, from_cap, slope, per_scale;
     bool capped, sloped;
@@ -27,8 +27,9 @@ struct Scores {
     __device__ __forceinline__ void of_head(const Problem& p, int head) {
         if (sloped) slope = p.slopes[head] * per_scale;
     }
+    // `power`: of two, that both come times (0: none)
     template <typename Lse, typename Far>
-    __device__ __forceinline__ void weights(f32x16& x, f32x16& y, Lse lse, Far far) const {
+    __device__ __forceinline__ void weights(f32x16& x, f32x16& y, Lse lse, Far far, float power) const {
         if (capped) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -44,11 +45,50 @@ struct Scores {
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            x[e] = __builtin_amdgcn_exp2f(x[e] * factor);
+            x[e] = __builtin_amdgcn_exp2f(POWERS ? __builtin_fmaf(x[e], factor, power) : x[e] * factor);
             y[e] *= x[e];
         }
     }
 };
+
+// The power of two that ds of a lane's row (dQ) or key (dK) is taken times as an operand in f16, and that comes off the sums at the end: ds is
+// some size of <dO, V> / m, mostly below f16's normal numbers (6e-5), and with a large dO beyond its largest.  The largest
+// |<dO, V> - <dO, O>| of the first tile that has one, by which P <= 1 is multiplied yet, goes to 2^8: ds of a P of 2^-22 keeps all
+// its bits, and a later one has room for 2^7.  Should one be larger, the sums are not finite, and the walk that follows first looks for
+// the largest |ds|, which goes to 2^14 (scaling the sums down as it comes, as a softmax does, would not fit the registers: 550 to 700 us at
+// 4096 rows, 32 heads on 8, d = 128, f16).  bf16 has the powers of two of 32 bits.
+template <typename T>
+struct Fitted {
+    static constexpr bool kFits = T::kOne == F16::kOne;
+    static constexpr unsigned kNone = 8u << 23;
+    unsigned inverse = kNone;  // as bits of a float
+    __device__ __forceinline__ bool wanted() const { return kFits && __any(inverse == kNone); }
+    __device__ __forceinline__ void put(float most, int power) {
+        most = max_of_halves(most);
+        if (inverse == kNone && most > 0.f && most < kInf) inverse = max((int)(__float_as_uint(most) >> 23) - power, 9) << 23;
+    }
+    __device__ __forceinline__ float power() const { return (float)(127 - (int)(inverse >> 23)); }
+    __device__ __forceinline__ float back() const { return kFits ? __uint_as_float(inverse) : 1.f; }
+    __device__ __forceinline__ s16x8 operand(const f32x16& y, int step, bool look) const {
+        if constexpr (!kFits) return rounded_operand<T>(y, step);
+        const float times = look ? 0.f : __uint_as_float((254u << 23) - inverse);
+        u32x4 r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            F16::v2 w;  // (one instruction each with its rounding: the product with a power of two is exact)
+            w[0] = (_Float16)__builtin_fmaf(y[8 * step + 2 * e], times, 0.f);
+            w[1] = (_Float16)__builtin_fmaf(y[8 * step + 2 * e + 1], times, 0.f);
+            r[e] = __builtin_bit_cast(unsigned, w);
+        }
+        return __builtin_bit_cast(s16x8, r);
+    }
+};
+__device__ __forceinline__ float largest(const f32x16& y) {
+    float most = fabsf(y[0]);
+#pragma unroll
+    for (int e = 1; e < 16; ++e) most = fmaxf(most, fabsf(y[e]));
+    return most;
+}
 
 // Which of a tile's 64 rows hold an entry that is not finite: a bit for each, the same in all lanes.
 template <typename T, typename L>
@@ -134,10 +174,12 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         p.rowsums[at] = none || !lost ? -lse : __builtin_nanf("");
         p.rowsums[(int64_t)p.hq * p.mask.n + at] = none ? 0.f : -rowsum;
     }
-    Scores<LARGE_CAP> to(p);
+    Scores<LARGE_CAP, Fitted<T>::kFits> to(p);
     if (see.inside) to.of_head(p, head);
 
     f32x16 sum[kBlocks];
+    Fitted<T> fitted;
+    float most = 0.f;  // |ds|, where a walk looks for it
     Lane<DP> at_lane(lane);
     unsigned char* const keys = lds;
     unsigned char* const values = lds + 2 * L::kBytes;
@@ -145,7 +187,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         for (int b = 0; b < kBlocks; ++b) sum[b] = f32x16{};
     };
     // One tile that lies in LDS, its rows as the last product takes them at `last_keys`.
-    auto tile_of = [&](int j0, const unsigned char* last_keys) {
+    auto tile_of = [&](int j0, const unsigned char* last_keys, bool look) {
         if (j0 >= high || j0 + kTileKeys <= low) return;
         const bool edge = j0 < all_low || j0 + kTileKeys > all_high;
 #pragma unroll
@@ -160,13 +202,19 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
                 x = T::mfma(at_lane.row(keys, t, k), q[k], x);
                 y = T::mfma(at_lane.row(values, t, k), g[k], y);
             }
+            if (fitted.wanted() && !look) fitted.put(largest(y), 8);
             const float away = (float)(see.at - j0 - 4 * half - 32 * t);
-            to.weights(x, y, [&](int) { return lse; }, [&](int e) { return away - (float)(8 * (e >> 2) + (e & 3)); });
+            to.weights(x, y, [&](int) { return lse; }, [&](int e) { return away - (float)(8 * (e >> 2) + (e & 3)); },
+                       look ? 0.f : fitted.power());
             if (edge) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if ((unsigned)(j0 + 4 * half + 32 * t + 8 * (e >> 2) + (e & 3) - see.lo) >= (unsigned)(see.hi - see.lo))
                         y[e] = 0.f;
+            }
+            if (look) {
+                most = fmaxf(most, largest(y));
+                y *= 0.f;
             }
             const s16x8 w0 = rounded_operand<T>(y, 0), w1 = rounded_operand<T>(y, 1);
 #pragma unroll
@@ -199,7 +247,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         for (int j0 = first; j0 < last; j0 += kTileKeys, buffer ^= L::kBytes, at_lane.other(L::kBytes)) {
             arrive_and_wait();
             if (j0 + kTileKeys < last) bring(j0 + kTileKeys, buffer ^ L::kBytes);
-            tile_of(j0, keys);
+            tile_of(j0, keys, false);
         }
         done = all_finite();
         at_lane = Lane<DP>(lane);
@@ -210,23 +258,27 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     // for the product with ds alone (the scores are made of what K holds), and keeps in mind which rows see one: of
     // those, and of no others, the gradient is NaN, as 0 * infinity is.
     for (; !done; ++entries) {
-        begin();
-        for (int j0 = first; j0 < last; j0 += kTileKeys) {
-            arrive_and_wait();
-            stage<T, DP, 256>(keys, p.k, kv, j0, first, last, p.d, tid, kAsTheyAre);
-            stage<T, DP, 256>(values, p.v, kv, j0, first, last, p.d, tid, kAsTheyAre);
-            if (entries == kFinite) stage<T, DP, 256>(keys + L::kBytes, p.k, kv, j0, first, last, p.d, tid, kFinite);
-            arrive_and_wait();
-            if (entries == kFinite) {
-                const uint64_t bad = not_finite<T, L>(keys, lane);
-                lost = lost || (bad & bits_between(see.lo - j0, see.hi - j0));
+        fitted = Fitted<T>();
+        for (int look = Fitted<T>::kFits && entries == kFinite; look >= 0; --look) {
+            begin();
+            for (int j0 = first; j0 < last; j0 += kTileKeys) {
+                arrive_and_wait();
+                stage<T, DP, 256>(keys, p.k, kv, j0, first, last, p.d, tid, kAsTheyAre);
+                stage<T, DP, 256>(values, p.v, kv, j0, first, last, p.d, tid, kAsTheyAre);
+                if (entries == kFinite) stage<T, DP, 256>(keys + L::kBytes, p.k, kv, j0, first, last, p.d, tid, kFinite);
+                arrive_and_wait();
+                if (entries == kFinite) {
+                    const uint64_t bad = not_finite<T, L>(keys, lane);
+                    lost = lost || (bad & bits_between(see.lo - j0, see.hi - j0));
+                }
+                tile_of(j0, entries == kFinite ? keys + L::kBytes : keys, look);
             }
-            tile_of(j0, entries == kFinite ? keys + L::kBytes : keys);
+            if (look) fitted.put(most, 14);
         }
         done = entries == kFinite || all_finite();
     }
     if (!see.inside) return;
-    const float times = none ? 0.f : lost ? __builtin_nanf("") : p.scale;
+    const float times = none ? 0.f : lost ? __builtin_nanf("") : p.scale * fitted.back();
     if (none) begin();
     if (p.row_splits > 1) {
         float* const parts = p.row_partial + (split * (int64_t)p.hq * p.mask.n + at) * p.d;
@@ -296,6 +348,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     }
 
     f32x16 dk[kBlocks], dv[kBlocks];
+    Fitted<T> fitted;  // of dk
+    float most = 0.f;
     Lane<DP> at_lane(lane);
     // This part's steps, of those through all rows of all heads that read K and V: from row0 of head0 to before row1 of the
     // last head.
@@ -315,8 +369,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     const int from_key = see.at - key + 4 * half, from_first = 4 * half - see.lo;
     const unsigned seen = see.hi - see.lo;
     // 32 rows that lie in LDS.
-    Scores<LARGE_CAP> to(p);
-    auto tile_of = [&](int i0, int buffer) {
+    Scores<LARGE_CAP, false> to(p);
+    auto tile_of = [&](int i0, int buffer, bool look) {
         if (i0 >= high || i0 + kStepRows <= low) return;
         const unsigned own = at_lane.rows ^ (buffer ? L::kBytes : 0);
         auto own_at = [&](int c) { return *reinterpret_cast<const s16x8*>(own_values + (own ^ (32 * c))); };
@@ -337,17 +391,19 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
             y = T::mfma(at_lane.row(grads, 0, c), own_at(c), y);
             if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         }
+        if (fitted.wanted() && !look) fitted.put(largest(y), 8);
         const float away = (float)(i0 + from_key);
         to.weights(x, y, [&](int e) { return -of_rows[buffer][0][8 * (e >> 2) + 4 * half + (e & 3)]; },
-                   [&](int e) { return away + (float)(8 * (e >> 2) + (e & 3)); });
+                   [&](int e) { return away + (float)(8 * (e >> 2) + (e & 3)); }, 0.f);
         if (i0 < all_low || i0 + kStepRows > all_high) {
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 if ((unsigned)(i0 + from_first + 8 * (e >> 2) + (e & 3)) >= seen) x[e] = y[e] = 0.f;
         }
+        if (look) most = fmaxf(most, largest(y));
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            const s16x8 weights = rounded_operand<T>(x, c), slopes = rounded_operand<T>(y, c);
+            const s16x8 weights = rounded_operand<T>(x, c), slopes = fitted.operand(y, c, look);
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
                 dv[b] = T::mfma(at_lane.column(grads, b, c), weights, dv[b]);
@@ -388,7 +444,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
                     bring(head, i0 + kStepRows, buffer ^ 1);
                 else if (head + 1 < head1)
                     bring(head + 1, first, buffer ^ 1);
-                tile_of(i0, buffer);
+                tile_of(i0, buffer, false);
             }
         }
         done = all_finite();
@@ -398,18 +454,22 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     // Entries of Q and dO that are not finite as zeros in a second walk.  Their rows have a log-sum that the walk by rows
     // has made NaN, and with it P (or minus infinity, and P = 0).
     for (; !done; ++entries) {
-        begin();
-        for (int head = head0; head < head1; ++head) {
-            to.of_head(p, head);
-            const int end = head + 1 < head1 ? last : row1;
-            for (int i0 = head == head0 ? row0 : first; i0 < end; i0 += kStepRows) {
-                arrive_and_wait();
-                stage<T, DP, 256, kStepRows>(queries, p.q, head, i0, first, last, p.d, tid, entries);
-                stage<T, DP, 256, kStepRows>(grads, p.dO, head, i0, first, last, p.d, tid, entries);
-                if (wave < 2 && lane < kStepRows) of_rows[0][wave][lane] = i0 + lane < last ? sums_of(wave, head, i0)[lane] : 0.f;
-                arrive_and_wait();
-                tile_of(i0, 0);
+        fitted = Fitted<T>();
+        for (int look = Fitted<T>::kFits && entries == kFinite; look >= 0; --look) {
+            begin();
+            for (int head = head0; head < head1; ++head) {
+                to.of_head(p, head);
+                const int end = head + 1 < head1 ? last : row1;
+                for (int i0 = head == head0 ? row0 : first; i0 < end; i0 += kStepRows) {
+                    arrive_and_wait();
+                    stage<T, DP, 256, kStepRows>(queries, p.q, head, i0, first, last, p.d, tid, entries);
+                    stage<T, DP, 256, kStepRows>(grads, p.dO, head, i0, first, last, p.d, tid, entries);
+                    if (wave < 2 && lane < kStepRows) of_rows[0][wave][lane] = i0 + lane < last ? sums_of(wave, head, i0)[lane] : 0.f;
+                    arrive_and_wait();
+                    tile_of(i0, 0, look);
+                }
             }
+            if (look) fitted.put(most, 14);
         }
         done = entries == kFinite || all_finite();
     }
@@ -419,6 +479,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     asm("" : "+v"(tid_again));
     const int half_again = (tid_again >> 5) & 1;
     const int64_t row = tile * kTileRows + (tid_again >> 6) * 32 + (tid_again & 31);
+    const float times = p.scale * fitted.back();
     if (p.splits > 1) {
         const int64_t keys = (int64_t)p.mask.m * p.hkv;
         float* const o = p.partial + (2 * part * keys + row * p.hkv + kv) * p.d;
@@ -426,7 +487,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
-                put4(o, 32 * b + 8 * a + 4 * half_again, p.d, dk[b] * p.scale, 4 * a);
+                put4(o, 32 * b + 8 * a + 4 * half_again, p.d, dk[b] * times, 4 * a);
                 put4(o + keys * p.d, 32 * b + 8 * a + 4 * half_again, p.d, dv[b], 4 * a);
             }
         return;
@@ -438,7 +499,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
             float x[4], y[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[e] = dk[b][4 * a + e] * p.scale;
+                x[e] = dk[b][4 * a + e] * times;
                 y[e] = dv[b][4 * a + e];
             }
             put4<T>(p.dk.data + row * p.dk.ld + kv * p.dk.hs, 32 * b + 8 * a + 4 * half_again, p.d, p.dk.wide, x);

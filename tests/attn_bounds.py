@@ -6,8 +6,8 @@ Bounds, u = eps / 2 of the type:
               score itself (the kernels have two forms of tanh); slopes and the exponential a few steps of what they act on
   a weight    rounded once to the type, f16 with its powers of two moved up: by 2^7 and more above the largest one,
               so that half of the smallest step, 2^-25, is 2^-32 of it; in dV by 2^14: 2^-39
-  ds          rounded once to the type, f16 times a power of two that puts the largest one of the row (dQ) or the key (dK)
-              at 2^7 or more: half of the smallest step is 2^-32 of that largest one
+  ds          rounded once to the type, f16 times a power of two that puts the largest |<dO, V> - <dO, O>| of some rows and keys at
+              2^8 or more, or the largest |ds| at 2^14: half of the smallest step is 2^-33 of the largest of all
 """
 import math
 
@@ -32,7 +32,7 @@ def attention(Q, K, V, dO=None, scale=None, causal=False, cap=0.0, slopes=None, 
     f16 = Q.dtype == torch.float16
     eps = torch.finfo(Q.dtype).eps / 2
     tiny = 2.0 ** -25 if f16 else 2.0 ** -134
-    small_P, small_dV, small_ds = (2.0 ** -32, 2.0 ** -39, 2.0 ** -32) if f16 else (2.0 ** -134, 2.0 ** -134, 0.0)
+    small_P, small_dV, small_ds = (2.0 ** -32, 2.0 ** -39, 2.0 ** -33) if f16 else (2.0 ** -134, 2.0 ** -134, 0.0)
     Q, K, V = (t.detach().double().cpu() for t in (Q, K, V))
     dO = None if dO is None else dO.detach().double().cpu()
     (n, hq, d), (m, hkv, _) = Q.shape, K.shape
@@ -56,6 +56,11 @@ def attention(Q, K, V, dO=None, scale=None, causal=False, cap=0.0, slopes=None, 
         for f in range(hkv):
             k, v = K[k0:k1, f], V[k0:k1, f]
             all_ds, all_off, all_q, all_seen = [], [], [], []
+            if dO is not None:  # |<dO, V> - <dO, O>| at most, by rows and heads, and by keys (O is a mean of V)
+                met = torch.nan_to_num(dO[:, f * group:(f + 1) * group].flatten(0, 1) @ V[:, f].T, 0, 0, 0).abs()
+                by_row = met.amax(1, keepdim=True) if m else torch.zeros(n * group, 1).double()
+                by_key = (met + by_row).amax(0)[k0:k1, None] if n else None
+                by_row = 2 * by_row.view(n, group)
             for name in ("dK", "dV"):
                 r[name][k0:k1, f] = 0.0
             for h in range(f * group, (f + 1) * group):
@@ -114,7 +119,7 @@ def attention(Q, K, V, dO=None, scale=None, causal=False, cap=0.0, slopes=None, 
                     off_ds = off_ds + torch.nan_to_num(P * raw.abs(), 0, 0, 0) * (2 * off / cap + 16 * STEP32)
                 off_ds = torch.where(seen, off_ds, torch.zeros_like(off_ds))
                 all_ds.append(ds), all_off.append(off_ds), all_q.append(q), all_seen.append(seen)
-                most = (fine + off_ds).amax(1, keepdim=True) if nk else torch.zeros(nq, 1).double()
+                most = by_row[q0:q1, h - f * group, None]
                 dQ = scale * _masked(ds, seen, k)
                 # one of K that is not finite: NaN in dQ of the rows that see it
                 meets = (seen & ~torch.isfinite(k).all(1)[None]).any(1)
@@ -127,12 +132,11 @@ def attention(Q, K, V, dO=None, scale=None, causal=False, cap=0.0, slopes=None, 
                 r["dV+"][k0:k1, f] += 1.01 * ((off_P + (nq * hq + 4) * STEP32 * torch.nan_to_num(P, 0)).T @ size_g)
             if dO is None or not nq or not nk:
                 continue
-            most = torch.cat([torch.nan_to_num(x, 0, 0, 0).abs() + o for x, o in zip(all_ds, all_off)]).amax(0)[:, None]
             for ds, off_ds, q, seen in zip(all_ds, all_off, all_q, all_seen):
                 size_q = torch.nan_to_num(q, 0, 0, 0).abs()
                 r["dK"][k0:k1, f] += scale * _masked(ds.T, seen.T, q)
                 r["dK+"][k0:k1, f] += 1.01 * scale * ((off_ds + (nq * hq + 4) * STEP32 * torch.nan_to_num(ds, 0, 0, 0).abs()).T @ size_q +
-                                                      small_ds * most * (seen.double().T @ size_q))
+                                                      small_ds * by_key * (seen.double().T @ size_q))
     for c in range(len(starts) - 1):  # a gradient that is not finite: whichever way
         for name, at in (("dQ", slice(starts[c], starts[c + 1])), ("dK", slice(k_starts[c], k_starts[c + 1])),
                          ("dV", slice(k_starts[c], k_starts[c + 1]))):

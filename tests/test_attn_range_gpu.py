@@ -1,4 +1,4 @@
-"""Attention over the whole range of what it accepts: entries that are not finite, caps of every size, on each way of reading rows and with the work in parts.  Values and bounds: attn_bounds.py."""
+"""Attention over the whole range of what it accepts: entries that are not finite, caps of every size, gradients of every magnitude, on each way of reading rows and with the work in parts.  Values and bounds: attn_bounds.py."""
 import pytest
 
 import paper_2206_14148_amd as A
@@ -144,3 +144,27 @@ def test_caps_of_every_size_over_the_cache(cap, code):
         score = d ** -0.5 * float(Q.abs().double().sum(3).max()) * float((k.abs().amax((2, 3)) * scales[0]).max())
         most = most + 4 * 16 * STEP32 * score * float((v.abs().amax((2, 3)) * scales[1]).max())
     assert ((got - O).abs() <= most).all(), ((got - O).abs() / most).max()
+
+
+# ---- magnitudes -----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("size", [1.0, 1e-2, 1e-3, 1e-4])
+def test_gradients_of_small_ones_in_f16(size):
+    """dO of a mean loss: ds is some size / m."""
+    check(*make(16, 4096, 2, 1, 128, "f16", 11, (1.0, 1.0, 1.0, size)))
+    check(*make(300, 2000, 2, 2, 64, "f16", 12, (1.0, 1.0, 1.0, size)), cap=30.0, starts=[0, 100, 300], k_starts=[0, 1500, 2000])
+    # larger K and Q, so that what comes out is not small itself
+    check(*make(40, 3000, 2, 1, 64, "f16", 13, (0.05, 20.0, 1.0, size)))
+
+
+def test_gradients_of_large_ones_in_f16():
+    """<dO, V> beyond the largest f16, gradients well within it."""
+    for causal in (False, True):
+        got, _, _ = check(*make(300, 300, 4, 2, 64, "f16", 14, (0.01, 0.01, 100.0, 1000.0)), causal=causal)
+        assert all(torch.isfinite(t).all() for t in got)
+    # rows of very different magnitudes, in either order
+    for turn in (False, True):
+        data = make(200, 260, 2, 1, 64, "f16", 15)
+        steps = torch.logspace(-6, 3, 200, device="cuda")[:, None, None]
+        data[3] = (data[3].float() * (steps.flip(0) if turn else steps)).half()
+        check(*data)
