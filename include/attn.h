@@ -119,8 +119,8 @@ knn_status attn_apply(const attn_rows_t *Q, const attn_rows_t *K, const attn_row
  *   dQ [n][hq][d], dK, dV [m][hkv][d]        DEVICE out, in the type of Q, overwritten
  *   workspace_bytes >= attn_grad_plan(...).workspace_bytes
  * Rows and keys outside the documents are left as they were.  P and ds are rounded to the type of Q for
- * the products (ds, which for a small dO or many keys lies below what f16 holds, times a power of two for every row and key), whose
- * sums are fp32 in a fixed order: no atomics, the same bits on every call.
+ * the products (in f16, where they lie below what it holds for many keys or a small dO, P times 2^14 and ds times a power of two for
+ * every row and key), whose sums are fp32 in a fixed order: no atomics, the same bits on every call.
  * Entries that are not finite.  One in a row's Q or dO (or O) makes its dQ, and dK and dV of the keys that it sees, not finite, one in K
  * the dQ of the rows that see it, and so on by the formulas where a score is NaN or +infinity (the row's log-sum is NaN); no others.
  * A row that sees no key, or whose scores are all -infinity, has dQ = 0 and adds nothing to the others.

@@ -65,7 +65,12 @@ struct Fitted {
     __device__ __forceinline__ bool wanted() const { return kFits && __any(inverse == kNone); }
     __device__ __forceinline__ void put(float most, int power) {
         most = max_of_halves(most);
-        if (inverse == kNone && most > 0.f && most < kInf) inverse = max((int)(__float_as_uint(most) >> 23) - power, 9) << 23;
+        if (inverse == kNone && most > 0.f && most < kInf) inverse = min(max((int)(__float_as_uint(most) >> 23) - power, 9), 246) << 23;
+    }
+    // (a power that was not too much stays, and with it the bits of the results that did not need this walk)
+    __device__ __forceinline__ void put_again(float most) {
+        if (max_of_halves(most) > 0x1p15f * __uint_as_float(inverse)) inverse = kNone;
+        put(most, 14);
     }
     __device__ __forceinline__ float power() const { return (float)(127 - (int)(inverse >> 23)); }
     __device__ __forceinline__ float back() const { return kFits ? __uint_as_float(inverse) : 1.f; }
@@ -258,7 +263,6 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     // for the product with ds alone (the scores are made of what K holds), and keeps in mind which rows see one: of
     // those, and of no others, the gradient is NaN, as 0 * infinity is.
     for (; !done; ++entries) {
-        fitted = Fitted<T>();
         for (int look = Fitted<T>::kFits && entries == kFinite; look >= 0; --look) {
             begin();
             for (int j0 = first; j0 < last; j0 += kTileKeys) {
@@ -273,7 +277,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
                 }
                 tile_of(j0, entries == kFinite ? keys + L::kBytes : keys, look);
             }
-            if (look) fitted.put(most, 14);
+            if (look) fitted.put_again(most);
         }
         done = entries == kFinite || all_finite();
     }
@@ -369,7 +373,10 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     const int from_key = see.at - key + 4 * half, from_first = 4 * half - see.lo;
     const unsigned seen = see.hi - see.lo;
     // 32 rows that lie in LDS.
-    Scores<LARGE_CAP, false> to(p);
+    Scores<LARGE_CAP, Fitted<T>::kFits> to(p);
+    // P of f16 (of many keys some 1 / m, below its normal numbers from 16000 on) as an operand times 2^14, and ds with it.
+    constexpr int kPower = Fitted<T>::kFits ? 14 : 0;
+    constexpr float kBack = kPower ? 0x1p-14f : 1.f;
     auto tile_of = [&](int i0, int buffer, bool look) {
         if (i0 >= high || i0 + kStepRows <= low) return;
         const unsigned own = at_lane.rows ^ (buffer ? L::kBytes : 0);
@@ -391,10 +398,10 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
             y = T::mfma(at_lane.row(grads, 0, c), own_at(c), y);
             if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         }
-        if (fitted.wanted() && !look) fitted.put(largest(y), 8);
+        if (fitted.wanted() && !look) fitted.put(largest(y), 8 - kPower);
         const float away = (float)(i0 + from_key);
         to.weights(x, y, [&](int e) { return -of_rows[buffer][0][8 * (e >> 2) + 4 * half + (e & 3)]; },
-                   [&](int e) { return away + (float)(8 * (e >> 2) + (e & 3)); }, 0.f);
+                   [&](int e) { return away + (float)(8 * (e >> 2) + (e & 3)); }, (float)kPower);
         if (i0 < all_low || i0 + kStepRows > all_high) {
 #pragma unroll
             for (int e = 0; e < 16; ++e)
@@ -454,7 +461,6 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     // Entries of Q and dO that are not finite as zeros in a second walk.  Their rows have a log-sum that the walk by rows
     // has made NaN, and with it P (or minus infinity, and P = 0).
     for (; !done; ++entries) {
-        fitted = Fitted<T>();
         for (int look = Fitted<T>::kFits && entries == kFinite; look >= 0; --look) {
             begin();
             for (int head = head0; head < head1; ++head) {
@@ -469,7 +475,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
                     tile_of(i0, 0, look);
                 }
             }
-            if (look) fitted.put(most, 14);
+            if (look) fitted.put_again(most);
         }
         done = entries == kFinite || all_finite();
     }
@@ -479,7 +485,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     asm("" : "+v"(tid_again));
     const int half_again = (tid_again >> 5) & 1;
     const int64_t row = tile * kTileRows + (tid_again >> 6) * 32 + (tid_again & 31);
-    const float times = p.scale * fitted.back();
+    const float times = p.scale * kBack * fitted.back();
     if (p.splits > 1) {
         const int64_t keys = (int64_t)p.mask.m * p.hkv;
         float* const o = p.partial + (2 * part * keys + row * p.hkv + kv) * p.d;
@@ -488,7 +494,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
                 put4(o, 32 * b + 8 * a + 4 * half_again, p.d, dk[b] * times, 4 * a);
-                put4(o + keys * p.d, 32 * b + 8 * a + 4 * half_again, p.d, dv[b], 4 * a);
+                put4(o + keys * p.d, 32 * b + 8 * a + 4 * half_again, p.d, dv[b] * kBack, 4 * a);
             }
         return;
     }
@@ -500,7 +506,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 x[e] = dk[b][4 * a + e] * times;
-                y[e] = dv[b][4 * a + e];
+                y[e] = dv[b][4 * a + e] * kBack;
             }
             put4<T>(p.dk.data + row * p.dk.ld + kv * p.dk.hs, 32 * b + 8 * a + 4 * half_again, p.d, p.dk.wide, x);
             put4<T>(p.dv.data + row * p.dv.ld + kv * p.dv.hs, 32 * b + 8 * a + 4 * half_again, p.d, p.dv.wide, y);

@@ -45,7 +45,7 @@ def check(Q, K, V, dO, limit=GB, names=NAMES, **o):
 
 @pytest.mark.parametrize("reading", ["16 bytes", "entries"])
 @pytest.mark.parametrize("cap", [0.0, 20.0, 1e5])
-@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 96)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 128), ("bf16", 96)])
 def test_infinities_reach_the_gradients_of_who_meets_them(dtype, d, cap, reading):
     """An infinity in Q, K, V or dO, of either sign: not finite where it is met, whatever the scores come to, and
     nothing changed for the others."""
@@ -61,7 +61,7 @@ def test_infinities_reach_the_gradients_of_who_meets_them(dtype, d, cap, reading
             data = [t.clone() if reading == "16 bytes" else odd(t) for t in clean]
             data[which][row, head, 0] = value
             got, r, _ = check(*data, **o)
-            # whoever does not meet it has the same bits
+            # whoever does not meet it has the same bits (in f16 the power of two of ds goes by a tile's entries, met or not)
             document = (0, 90) if row < 90 else (90, 200)
             heads = range(4) if which in (0, 3) else (2 * head, 2 * head + 1)
             heads = [head] if which in (0, 3) else list(heads)
@@ -71,12 +71,14 @@ def test_infinities_reach_the_gradients_of_who_meets_them(dtype, d, cap, reading
                 q_met[(row if which in (0, 3) else row):(row + 1 if which in (0, 3) else document[1]), h] = True
             k_met[document[0]:document[1], kv] = True
             for name, a, b, met in zip(NAMES, got, first, (q_met, q_met.T, q_met, k_met, k_met)):
+                if dtype == "f16" and name in ("dQ", "dK"):
+                    continue
                 same = (a == b) | (torch.isnan(a) & torch.isnan(b))
                 same = same.cpu() if name == "lse" else same.all(2).cpu()
                 assert (same | met).all(), (which, value, name)
 
 
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("cap", [0.0, 20.0])
 def test_infinities_where_the_work_is_in_parts(dtype, cap):
     n, m, d = 6, 3000, 64
@@ -116,7 +118,7 @@ def test_rows_whose_scores_are_all_minus_infinity():
 CAPS = [0.5, 64.0, 65.0, 300.0, 1e4, 1e6, 1e9, 2.0 ** 60]
 
 
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("cap", CAPS)
 def test_caps_of_every_size(cap, dtype):
     for d, size in ((64, 1.0), (128, 3.0), (80, 40.0)):
@@ -168,3 +170,8 @@ def test_gradients_of_large_ones_in_f16():
         steps = torch.logspace(-6, 3, 200, device="cuda")[:, None, None]
         data[3] = (data[3].float() * (steps.flip(0) if turn else steps)).half()
         check(*data)
+
+
+def test_dv_of_many_keys_in_f16():
+    """Weights of 4e-6 each, far below f16's normal numbers."""
+    check(*make(4, 1 << 18, 1, 1, 64, "f16", 16, (0.1, 1.0, 1.0, 100.0)))
