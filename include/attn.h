@@ -102,8 +102,8 @@ knn_status attn_grad_plan(int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t
  * Rows before the first document or behind the last are not written; what they and keys there hold has no
  * influence.  Scores, maxima, totals and sums are fp32; a tile's probabilities are rounded to the type of V
  * for their product with it, and O is rounded once.  Every sum has a fixed order.
- * An entry that is not finite (NaN in Q; infinite or NaN in K or V) reaches the rows that see it and
- * no others.  A row whose scores are all -infinity counts as one that sees no key.
+ * An entry that is not finite (NaN in Q; infinite or NaN in K or V) reaches the rows that see it, one of V however
+ * small its weight, and no others.  A row whose scores are all -infinity counts as one that sees no key.
  */
 knn_status attn_apply(const attn_rows_t *Q, const attn_rows_t *K, const attn_rows_t *V, int64_t n, int64_t m,
                       int32_t hq, int32_t hkv, int32_t d, const attn_options_t *options, uint64_t mem_limit_bytes,

@@ -458,9 +458,9 @@ __device__ __forceinline__ Joined join_ranges(const float* partial, int ranges, 
         for (int s = 0; s < 8; ++s) {
             const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s0 + s));
             r.total += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(total), s0 + s));
-            // (zero times an infinity, of a range whose weights have vanished against another's: nothing)
-            r.x[0] = __builtin_fmaf(fs != 0.f ? a[s] : 0.f, fs, r.x[0]);
-            r.x[1] = __builtin_fmaf(fs != 0.f ? b[s] : 0.f, fs, r.x[1]);
+            // (an infinity of a range whose weights have vanished against another's is one all the same)
+            r.x[0] = __builtin_fmaf(a[s], fabsf(a[s]) < kInf ? fs : 1.f, r.x[0]);
+            r.x[1] = __builtin_fmaf(b[s], fabsf(b[s]) < kInf ? fs : 1.f, r.x[1]);
         }
     }
     if constexpr (WAVES > 1) {
@@ -479,8 +479,9 @@ __device__ __forceinline__ Joined join_ranges(const float* partial, int ranges, 
         for (int w = 0; w < WAVES; ++w) {
             const float fw = __builtin_amdgcn_exp2f(of_wave[w][128] - r.top);
             r.total = __builtin_fmaf(of_wave[w][129], fw, r.total);
-            r.x[0] = __builtin_fmaf(fw != 0.f ? of_wave[w][lane] : 0.f, fw, r.x[0]);
-            r.x[1] = __builtin_fmaf(fw != 0.f ? of_wave[w][64 + lane] : 0.f, fw, r.x[1]);
+            const float a = of_wave[w][lane], b = of_wave[w][64 + lane];
+            r.x[0] = __builtin_fmaf(a, fabsf(a) < kInf ? fw : 1.f, r.x[0]);
+            r.x[1] = __builtin_fmaf(b, fabsf(b) < kInf ? fw : 1.f, r.x[1]);
         }
     }
     return r;

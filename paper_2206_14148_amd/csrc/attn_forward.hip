@@ -178,12 +178,18 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
             for (int t = 0; t < 2; ++t) x[t] -= up;
         }
     };
-    // One tile that lies in LDS.
-    auto tile_of = [&](int j0) {
+    // One tile that lies in LDS.  marks: with a weight of one for every key that is seen (and has a score above -infinity).
+    auto tile_of = [&](int j0, bool marks) {
         if (j0 >= high || j0 + kTileKeys <= low) return;
         f32x16 x[2];
         products(x);
         scores(x, j0);
+        if (marks) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[t][e] = x[t][e] > -kInf ? 0.f : -kInf;
+        }
         s16x8 weights[4];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -227,7 +233,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
         for (int s = s0; s < s1; ++s, at.other(L::kBytes)) {
             arrive_and_wait();
             if (s + 1 < s1) bring(s + 1);
-            tile_of(first + s * kTileKeys);
+            tile_of(first + s * kTileKeys, false);
         }
         if (all_finite()) {
             write(entries);
@@ -239,7 +245,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     // Without 16-byte reads; and where a sum came out not finite.  An infinity or a NaN in V meets the zero weights of
     // rows that do not see it as well, and 0 * infinity is NaN.  Then the workgroup walks three times more: with those
     // entries as zeros, and with ones for what raises a sum to +infinity and to -infinity, whose sums are not zero
-    // for the rows that see one.
+    // for the rows that see one (all weights are one there: a small one may round to zero, and still carries an infinity).
     for (;; ++entries) {
         begin();
         for (int s = s0; s < s1; ++s) {
@@ -248,7 +254,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
             stage<T, DP, 256>(keys, p.k, kv, j0, first, last, p.d, tid, kAsTheyAre);
             stage<T, DP, 256>(values, p.v, kv, j0, first, last, p.d, tid, entries);
             arrive_and_wait();
-            tile_of(j0);
+            tile_of(j0, entries >= kUp);
         }
         if (entries == kAsTheyAre && !all_finite()) continue;
         write(entries);

@@ -98,6 +98,27 @@ def test_infinities_where_the_work_is_in_parts(dtype, cap):
         check(*data, cap=cap)
 
 
+@pytest.mark.parametrize("reading", ["16 bytes", "entries"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_infinities_of_v_behind_small_weights(dtype, reading):
+    """Scores 20, 60 and 200 apart: a weight that rounds to nothing still carries an infinity or a NaN."""
+    for n, m in ((5, 100), (3, 3000)):
+        for away in (20.0, 60.0, 200.0):
+            Q, K, V, _ = make(n, m, 2, 1, 64, dtype, 7)
+            Q.zero_(), K.zero_()
+            Q[:, :, 0] = 8.0
+            K[:, :, 0] = -away
+            K[7, :, 0] = 0.0
+            for value in (INF, -INF, float("nan")):
+                W = V.clone()
+                W[m - 30, 0, 5] = value
+                W[11, 0, 9] = value
+                if reading == "entries":
+                    check(odd(Q), odd(K), odd(W), None, names=NAMES[:2])
+                else:
+                    check(Q, K, W, None, names=NAMES[:2])
+
+
 def test_rows_whose_scores_are_all_minus_infinity():
     """They count as rows that see no key, with an infinity of their own as well."""
     for which in (0, 1):
