@@ -5,8 +5,14 @@ namespace attn {
 
 namespace {
 
-// The largest score of a row may grow by this many powers of two before its sums are scaled down to it.
-constexpr float kSlack = 8.f;
+// A row's weights are powers of two of its scores less `top`, which goes up so that the largest is 2^kPower when it is over 2^kSlack.
+// bf16: that is, sums are scaled down for a score that grows by 8.  f16: its largest powers of two are used, so that a weight of 2^-21 of
+// the row's largest keeps all its bits (many small ones beside a large one add up: with kPower = 0 60000 weights of
+// 2^-24.5 came to 1.4 times their sum).
+template <typename T>
+constexpr float kPower = T::kOne == F16::kOne ? 7.f : 0.f;
+template <typename T>
+constexpr float kSlack = 8.f + kPower<T>;
 
 // A lane's sums of its row to memory, or to the workspace as they are.  entries: see the walk below.
 template <typename T, int BLOCKS>
@@ -105,7 +111,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     const bool capped = LARGE_CAP || p.cap > 0.f;
     const float to_cap = LARGE_CAP ? p.scale / p.cap : capped ? 2.f * factor / p.cap : 0.f, from_cap = p.cap / p.scale;
     const float slope = p.slopes && see.inside ? p.slopes[head] / p.scale : 0.f;
-    const float slack = kSlack / factor;
+    const float slack = kSlack<T> / factor, lift = kPower<T> / factor;
 
     f32x16 sum[kBlocks];
     float top, total;  // of a lane's row: what its scores are taken less of, the sum of its weights (of half the keys)
@@ -167,7 +173,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
         most = max_of_halves(most);
         if (__any(most > most_over)) {
             const bool none = most_over != slack;
-            const float up = none ? (most == -kInf ? 0.f : most) : fmaxf(most, 0.f);
+            const float up = none ? (most == -kInf ? 0.f : most - lift) : fmaxf(most - lift, 0.f);
             const float shrink = none ? 1.f : __builtin_amdgcn_exp2f(-up * factor);
             if (most > -kInf) most_over = slack;
             top += up;
@@ -193,13 +199,15 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
         s16x8 weights[4];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
+            float part = 0.f;  // (16 are added up before they meet what may be much larger)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 x[t][e] = __builtin_amdgcn_exp2f(x[t][e] * factor);
-                total += x[t][e];
+                part = e ? part + x[t][e] : x[t][e];
             }
             weights[2 * t] = rounded_operand<T>(x[t], 0);
             weights[2 * t + 1] = rounded_operand<T>(x[t], 1);
+            total += part;
         }
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)

@@ -1,4 +1,5 @@
-"""Attention over the whole range of what it accepts: entries that are not finite, caps of every size, gradients of every magnitude, on each way of reading rows and with the work in parts.  Values and bounds: attn_bounds.py."""
+"""Attention over the whole range of what it accepts: entries that are not finite, caps of every size, gradients and
+weights of every magnitude, on each way of reading rows and with the work in parts.  Values and bounds: attn_bounds.py."""
 import pytest
 
 import paper_2206_14148_amd as A
@@ -196,3 +197,15 @@ def test_gradients_of_large_ones_in_f16():
 def test_dv_of_many_keys_in_f16():
     """Weights of 4e-6 each, far below f16's normal numbers."""
     check(*make(4, 1 << 18, 1, 1, 64, "f16", 16, (0.1, 1.0, 1.0, 100.0)))
+
+
+@pytest.mark.parametrize("limit", [GB, 0])
+def test_many_small_weights_beside_a_large_one_in_f16(limit):
+    """One key of weight 1 and value 0, 60000 of weight 2^-24.5 and value 1: what they add up to counts."""
+    m = 60_000
+    Q, K, V, _ = make(2, m, 1, 1, 64, "f16", 17)
+    Q.zero_(), K.zero_()
+    Q[:, :, 0], K[:, :, 0] = 8.0, -17.0
+    V.fill_(1.0)
+    K[777], V[777] = 0.0, 0.0
+    check(Q, K, V, None, limit=limit, names=NAMES[:2])
