@@ -439,6 +439,8 @@ __device__ __forceinline__ Joined join_ranges(const float* partial, int ranges, 
     float most = top;
 #pragma unroll
     for (int s = 32; s; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+    // (parts that are finite each may add up past the largest number: 256 of them do not where each comes times 2^-8)
+    if (most > -kInf) most += 8.f;
     const float base = most == -kInf ? 0.f : most;
     const float f = __builtin_amdgcn_exp2f(top - base);
     total *= f;

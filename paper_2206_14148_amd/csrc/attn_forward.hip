@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     const bool capped = LARGE_CAP || p.cap > 0.f;
     const float to_cap = LARGE_CAP ? p.scale / p.cap : capped ? 2.f * factor / p.cap : 0.f, from_cap = p.cap / p.scale;
     const float slope = p.slopes && see.inside ? p.slopes[head] / p.scale : 0.f;
-    const float slack = kSlack<T> / factor, lift = kPower<T> / factor;
+    float slack = kSlack<T> / factor, lift = kPower<T> / factor;
 
     f32x16 sum[kBlocks];
     float top, total;  // of a lane's row: what its scores are taken less of, the sum of its weights (of half the keys)
@@ -221,13 +221,14 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     };
 
     int entries = kAsTheyAre;
+    float zero;  // NaN where a lane's sums are not finite
     auto all_finite = [&]() {
-        float zero = 0.f;
+        zero = 0.f;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(sum[b][e], 0.f, zero);
-        return !__syncthreads_or(zero != 0.f);  // (NaN)
+        return !__syncthreads_or(zero != 0.f);
     };
     if (p.k.wide && p.v.wide) {
         // one pair of buffers is worked on while the other is filled
@@ -254,7 +255,9 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
     // rows that do not see it as well, and 0 * infinity is NaN.  Then the workgroup walks three times more: with those
     // entries as zeros, and with ones for what raises a sum to +infinity and to -infinity, whose sums are not zero
     // for the rows that see one (all weights are one there: a small one may round to zero, and still carries an infinity).
-    for (;; ++entries) {
+    // In bf16 values near the largest number may add up past it though their mean is finite.  Rows whose sums are not finite without
+    // such entries either are made again with weights of 2^-32 at most, of which the 2^30 keys there can be add up to 1 / 4.
+    for (bool low = false, mine = true;;) {
         begin();
         for (int s = s0; s < s1; ++s) {
             const int j0 = first + s * kTileKeys;
@@ -264,9 +267,22 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
             arrive_and_wait();
             tile_of(j0, entries >= kUp);
         }
-        if (entries == kAsTheyAre && !all_finite()) continue;
-        write(entries);
+        const bool fine = entries >= kUp || all_finite();
+        if (entries == kAsTheyAre && !fine) {
+            entries = kFinite;
+            continue;
+        }
+        if (mine) write(entries);
         if (entries == kAsTheyAre || entries == kDown) return;
+        if (entries == kFinite && !fine && !low && kPower<T> == 0.f) {  // (f16 has no such values)
+            low = true;
+            slack = (kSlack<T> - 40.f) / factor;
+            lift = -40.f / factor;
+            mine = sum_of_halves(zero) != 0.f;
+            continue;
+        }
+        mine = true;
+        ++entries;
     }
 }
 

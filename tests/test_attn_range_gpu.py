@@ -209,3 +209,12 @@ def test_many_small_weights_beside_a_large_one_in_f16(limit):
     V.fill_(1.0)
     K[777], V[777] = 0.0, 0.0
     check(Q, K, V, None, limit=limit, names=NAMES[:2])
+
+
+def test_values_near_the_largest_number():
+    """Sums of weights that are not yet divided by their total, of values whose mean is finite."""
+    for n, m in ((70, 300), (2, 4000)):
+        Q, K, V, _ = make(n, m, 2, 1, 64, "bf16", 18)
+        V = (1e38 * (1 + 0.5 * torch.tanh(V.float()))).bfloat16()
+        got, _, _ = check(Q, K, V, None, names=NAMES[:2])
+        assert torch.isfinite(got[0]).all()
