@@ -218,8 +218,8 @@ knn_status attn_cache_plan(int64_t batch, int32_t nq, int32_t hq, int32_t hkv, i
  *   table [batch][width], lengths [batch]   DEVICE in, int32.  Tokens whose table entry is no block of the cache
  *                  are not seen; a length is at most width * block.
  *   scale, cap, slopes   as in attn_options_t
- * Scores, maxima, totals and sums are fp32.  A code is exact in 16 bits; probabilities are rounded to f16, times
- * the ratio of their block's scale to the largest of 64 tokens' scales.
+ * Scores, maxima, totals and sums are fp32 (values times their number of tokens below 2^127).  A code is exact in 16 bits;
+ * probabilities are rounded to f16, times the ratio of their block's scale to the largest of 64 tokens' scales, times 2^14.
  */
 knn_status attn_cache_apply(const attn_cache_t *cache, int32_t dtype, const attn_rows_t *Q, int64_t batch, int32_t nq,
                             int32_t hq, const int32_t *table, int64_t width, const int32_t *lengths, double scale,

@@ -485,7 +485,9 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheProblem p) {
         }
         float vmost = fmaxf(vs, __shfl_xor(vs, 16));
         vmost = fmaxf(vmost, __shfl_xor(vmost, 32));
-        const float share = vmost > 0.f ? vs / vmost : 0.f;
+        // A weight is at most one.  As an operand it comes times its block's scale over the largest of these tokens', and times 2^14:
+        // down to 2^-28 of weight and scales together an f16 keeps all its bits.
+        const float share = vmost > 0.f ? vs / vmost * 0x1p14f : 0.f;
 #pragma unroll
         for (int s = 0; s < SETS; ++s) {
             f32x4 x[4];
@@ -542,13 +544,15 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheProblem p) {
                 for (int t = 0; t < kTiles; ++t) sum[s][t] *= shrink;
             }
             const float base = top[s] == -kInf ? 0.f : top[s];
+            float part;  // (16 are added up before they meet what may be much larger)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     x[t][e] = __builtin_amdgcn_exp2f(x[t][e] - base);
-                    total[s] += x[t][e];
+                    part = t + e ? part + x[t][e] : x[t][e];
                 }
+            total[s] += part;
             f16x8 weights[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -560,7 +564,7 @@ __global__ __launch_bounds__(256) void attn_cache_kernel(CacheProblem p) {
                 y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<E4M3>(u32x2{vc[t][0], vc[t][1]}), weights[0], y, 0, 0, 0);
                 y = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves_of<E4M3>(u32x2{vc[t][2], vc[t][3]}), weights[1], y, 0, 0, 0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[s][t][e] = __builtin_fmaf(y[e], vmost, sum[s][t][e]);
+                for (int e = 0; e < 4; ++e) sum[s][t][e] = __builtin_fmaf(y[e] * 0x1p-14f, vmost, sum[s][t][e]);
             }
         }
     }

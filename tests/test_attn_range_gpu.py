@@ -218,3 +218,29 @@ def test_values_near_the_largest_number():
         V = (1e38 * (1 + 0.5 * torch.tanh(V.float()))).bfloat16()
         got, _, _ = check(Q, K, V, None, names=NAMES[:2])
         assert torch.isfinite(got[0]).all()
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+def test_cache_blocks_of_very_different_scales(code):
+    """A block of small values that has nearly all weight beside one of large values that has none."""
+    d, hq, block = 64, 2, 16
+    cache = A.AttnCache.empty(4, 1, d, block, code)
+    gen = torch.Generator().manual_seed(5)
+    K, V = torch.ones(64, 1, d), torch.randn(64, 1, d, generator=gen)
+    K[16:32] = -1.0
+    V[:16] *= 1e-3
+    V[16:32] *= 1e4
+    V[32:] *= 1e-3
+    A.attn_cache_append(cache, K.bfloat16().cuda(), V.bfloat16().cuda(), torch.arange(64, device="cuda"))
+    for size in (1.5, 2.5):
+        Q = torch.full((1, 1, hq, d), size, dtype=torch.bfloat16, device="cuda")
+        got = A.attn_cache_apply(Q, cache, words([[0, 1, 2, 3]]), words([64]), GB).double().cpu()
+        k, v = cache.k.cpu().float().double(), cache.v.cpu().float().double()
+        O, _ = F.cache_attention(Q, k, v, cache.k_scale.cpu(), cache.v_scale.cpu(), [[0, 1, 2, 3]], [64], d, block)
+        vv = (v[:, 0] * cache.v_scale.cpu().double()[:, :, None]).transpose(1, 2).reshape(64, d)
+        u = size * d ** -0.5 * (k[:, 0] * cache.k_scale.cpu().double()[:, :, None]).sum(2).view(64)
+        P = torch.softmax(u, 0)
+        err = STEP32 * (d + 24) * float(u.abs().max())
+        # weights in f16, a step of 2^-24 at the least, 2^14 times as large, in units of the largest scale
+        most = (2.0 ** -11 + 4 * err) * (P @ vv.abs()) + 2.0 ** -39 * 127 * float(cache.v_scale.max()) * 64 + 2.0 ** -9 * O.abs()
+        assert ((got - O).abs() <= 1.01 * most).all(), ((got - O).abs() / most).max()
