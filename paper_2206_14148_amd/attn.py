@@ -394,7 +394,7 @@ def attn_cache_map(lengths, news, table, free, block: int, n_slots: int, out=Non
 def attn_cache_append(cache: AttnCache, K, V, slots) -> None:
     """attn_cache_append(cache, K[count,hkv,d], V[count,hkv,d], slots int64 [count]): new rows into the cache.
 
-    The slots of one block must stand together; -1 is passed over.  A block's scale grows with its largest magnitude,
+    The slots of one block must stand together; -1 is passed over, within a block as well.  A block's scale grows with its largest magnitude,
     codes that it holds already follow; a block that gets its token 0 is begun anew.
     """
     c = cache._struct()

@@ -160,9 +160,12 @@ __device__ __forceinline__ float quotient_of(float code, float from, float to) {
 // search of the largest magnitude to the codes where they fit, else read again.  A block's codes of V lie across its rows, so
 // they are put together in LDS and written a word of four tokens at a time; a word that the run fills in part, and that is not
 // begun anew, is written byte by byte.
+// e4m3 needs few enough registers for a fifth wave on a SIMD (append of 8 prompts of up to 2048 rows, blocks of 64: 136 us with the
+// values that are looked at, 144 with four).
 constexpr int kAppendPasses = 4;
+constexpr int kAhead = 8;  // loads of slots under way together where rows without a place are passed over
 template <typename T, bool E4M3, int THREADS>
-__global__ __launch_bounds__(THREADS) void attn_append_kernel(AppendProblem p, int tokens) {
+__global__ __launch_bounds__(THREADS, E4M3 ? 5 : 4) void attn_append_kernel(AppendProblem p, int tokens) {
     const Cache& c = p.cache;
     extern __shared__ __attribute__((aligned(16))) unsigned char turned[];  // [row][block + 4]
     __shared__ int last_of[256];               // the last row of the run that goes to each token, -1: none
@@ -170,52 +173,94 @@ __global__ __launch_bounds__(THREADS) void attn_append_kernel(AppendProblem p, i
     __shared__ unsigned covered[8];            // tokens of the block that the run writes
     __shared__ unsigned char moved_to[2][256];  // what becomes of each code that the block holds
     __shared__ float of_wave[2][THREADS / 64];
-    __shared__ int run_end;
+    __shared__ int run_end, run_last, run_hole;
     const int tid = threadIdx.x;
     const int head = blockIdx.x % c.hkv, shift = __builtin_ctz(c.block), pitch = c.block + 4;
     const int64_t group = (int64_t)(blockIdx.x / c.hkv) * tokens, slots = c.blocks << shift;
-    auto block_of = [&](int64_t t) {
+    auto block_of = [&](int64_t t) {  // -1: none
         const int64_t s = t >= 0 && t < p.count ? p.slots[t] : -1;
-        return s >= 0 && s < slots ? s >> shift : -1;
+        return s >= 0 && s < slots ? (int)(s >> shift) : -1;
     };
     // lane l of each wave: whether a run begins at row group + l
-    const int64_t mine = (tid & 63) < tokens ? block_of(group + (tid & 63)) : -1;
-    const int64_t before_mine = (tid & 63) < tokens ? block_of(group + (tid & 63) - 1) : -1;
+    const int lane = tid & 63;
+    const int mine = lane < tokens ? block_of(group + lane) : -1;
+    int before_mine = lane < tokens ? block_of(group + lane - 1) : -1;
+    if (__any(mine >= 0 && before_mine < 0 && group + lane > 0)) {
+        // Rows without a place are passed over, however many: what counts is the last one before that has one, of this group or of those before.
+        const unsigned long long placed = __ballot(mine >= 0);
+        int before = -1;
+        unsigned long long found = 0;
+        for (int64_t t = group - 1; !found && t >= 0; t -= kAhead * 64) {
+            int b[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) b[k] = block_of(t - 64 * k - lane);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (!found) {
+                    before = b[k];
+                    found = __ballot(before >= 0);
+                }
+        }
+        before = found ? __shfl(before, __builtin_ctzll(found)) : -1;
+        const unsigned long long below = placed & ((1ull << lane) - 1);
+        before_mine = __shfl(mine, below ? 63 - __builtin_clzll(below) : 0);
+        if (!below) before_mine = before;
+    }
     unsigned long long firsts = __ballot(mine >= 0 && mine != before_mine);
     const int pieces = c.row / 8, per_pass = THREADS / pieces, piece = tid % pieces, line = tid / pieces;
     while (firsts) {
-        const int64_t first = group + __builtin_ctzll(firsts), block = block_of(first), at = block * c.hkv + head;
+        const int64_t first = group + __builtin_ctzll(firsts);
+        const int block = block_of(first);
+        const int64_t at = (int64_t)block * c.hkv + head;
         firsts &= firsts - 1;
         __syncthreads();
         if (tid < 8) covered[tid] = 0;
-        if (tid == 0) run_end = INT_MAX;
+        if (tid == 0) run_end = run_hole = INT_MAX, run_last = 0;
         for (int i = tid; i < c.block; i += THREADS) last_of[i] = -1;
         const float scales[2] = {c.k_scale[at], c.v_scale[at]};
         __syncthreads();
-        int count = 0;  // rows of the run (slots may be given twice: it can be longer than a block)
-        for (;; count += THREADS) {
-            const int64_t t = first + count + tid;
-            const bool other = block_of(t) != block;
-            if (count == 0 && !other) token_of[tid] = (int)(p.slots[t] & (c.block - 1));
-            if constexpr (THREADS == 64) {
-                const unsigned long long others = __ballot(other);
-                if (others) {
-                    count += __builtin_ctzll(others);
-                    break;
+        // The run goes on to before the first row that has another place; `count` to behind its last row, `hole` is the first row
+        // without a place in between.  (Slots may be given twice: it can be longer than a block.)
+        int count = 1, hole = INT_MAX;
+        bool ended = false;
+        for (int from = 0; !ended; from += from ? kAhead * THREADS : THREADS) {
+            int b[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) b[k] = k == 0 || from ? block_of(first + from + k * THREADS + tid) : -1;
+            if (from == 0) token_of[tid] = b[0] == block ? (int)(p.slots[first + tid] & (c.block - 1)) : -1;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (ended || (k && !from)) continue;
+                const int wave_from = from + k * THREADS + (tid & ~63);
+                const unsigned long long ends = __ballot(b[k] != block && (b[k] >= 0 || first + wave_from + lane >= p.count));
+                int end = ends ? wave_from + __builtin_ctzll(ends) : INT_MAX;
+                if constexpr (THREADS > 64) {
+                    if (lane == 0 && ends) atomicMin(&run_end, end);
+                    __syncthreads();
+                    end = run_end;
                 }
-            } else {
-                if (other) atomicMin(&run_end, count + tid);
-                __syncthreads();
-                const int found = run_end;
-                __syncthreads();  // (before anyone lowers it again)
-                if (found != INT_MAX) {
-                    count = found;
-                    break;
+                const unsigned long long inside = end >= wave_from + 64 ? ~0ull : end <= wave_from ? 0 : (1ull << (end - wave_from)) - 1;
+                const unsigned long long own = __ballot(b[k] == block) & inside, none = __ballot(b[k] < 0) & inside;
+                if constexpr (THREADS > 64) {
+                    if (lane == 0 && own) atomicMax(&run_last, wave_from + 63 - __builtin_clzll(own));
+                    if (lane == 0 && none) atomicMin(&run_hole, wave_from + __builtin_ctzll(none));
+                    __syncthreads();  // (and before anyone lowers the end again)
+                } else {
+                    if (own) count = wave_from + 64 - __builtin_clzll(own);
+                    if (none && hole == INT_MAX) hole = wave_from + __builtin_ctzll(none);
                 }
+                ended = end != INT_MAX;
             }
         }
+        if constexpr (THREADS > 64) {
+            count = run_last + 1;
+            hole = run_hole;
+        }
+        const bool holes = hole < count;
         __syncthreads();
-        auto token = [&](int i) { return i < THREADS ? token_of[i] : (int)(p.slots[first + i] & (c.block - 1)); };
+        auto token = [&](int i) {  // -1: none
+            return i < THREADS ? token_of[i] : block_of(first + i) == block ? (int)(p.slots[first + i] & (c.block - 1)) : -1;
+        };
         u32x4 rows[2][kAppendPasses];
         auto read = [&](int i0) {
 #pragma unroll
@@ -234,8 +279,16 @@ __global__ __launch_bounds__(THREADS) void attn_append_kernel(AppendProblem p, i
             read(i0);
             for (int i = i0 + tid; i < min(i0 + round, count); i += THREADS) {
                 const int to = token(i);
+                if (to < 0) continue;
                 atomicOr(&covered[to >> 5], 1u << (to & 31));
                 atomicMax(&last_of[to], i);
+            }
+            if (holes) {
+#pragma unroll
+                for (int n = 0; n < kAppendPasses; ++n) {
+                    const int i = i0 + line * kAppendPasses + n;
+                    if (i < count && token(i) < 0) rows[0][n] = rows[1][n] = u32x4{0, 0, 0, 0};
+                }
             }
 #pragma unroll
             for (int x = 0; x < 2; ++x)

@@ -7,6 +7,7 @@ import paper_2206_14148_amd as A
 torch = pytest.importorskip("torch")
 import attn_formulas as F  # noqa: E402
 from attn_bounds import STEP32, attention, compare  # noqa: E402
+from test_attn_cache_gpu import check_append, filled, values  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 GB = 10 ** 9
@@ -244,3 +245,31 @@ def test_cache_blocks_of_very_different_scales(code):
         # weights in f16, a step of 2^-24 at the least, 2^14 times as large, in units of the largest scale
         most = (2.0 ** -11 + 4 * err) * (P @ vv.abs()) + 2.0 ** -39 * 127 * float(cache.v_scale.max()) * 64 + 2.0 ** -9 * O.abs()
         assert ((got - O).abs() <= 1.01 * most).all(), ((got - O).abs() / most).max()
+
+
+# ---- appends whose rows do not all have a place ---------------------------------------------
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("block", [16, 32, 64, 256])
+def test_rows_without_a_place_within_a_run_are_passed_over(block, code):
+    """-1, and slots behind the cache, before, within and behind the rows of a block: few and very many; what stands in those
+    rows does not count for the scale."""
+    d, hkv, blocks = 64, 2, 7
+    gen = torch.Generator().manual_seed(block)
+    for gaps in ((1,), (2, 1, 70), (300, 1, 2500), (64, 63, 65, 5000), (1, 1, 1, 1, 1, 1)):
+        slots, gap = [], 0
+        for b, begin, count in ((5, 0, block // 2 + 3), (2, 3, 4), (6, block - 1, 1), (0, 0, block), (3, 1, 1), (1, 0, 1)):
+            for t in range(count):
+                if t in (0, 1, 2, count - 1):
+                    slots += [(-1, blocks * block, 1 << 40, -7)[gap % 4]] * gaps[gap % len(gaps)]
+                    gap += 1
+                slots.append(b * block + begin + t)
+        slots += [slots[-1]] + [-1] * gaps[-1]  # one given twice, then the rest of a padded step
+        cache = filled(blocks, hkv, d, block, code, 3)
+        K, V = (torch.randn(len(slots), hkv, d, generator=gen).half() for _ in range(2))
+        lost = torch.tensor([not 0 <= s < blocks * block for s in slots])
+        K[lost], V[lost] = 3000.0, -3000.0
+        check_append(cache, K.cuda(), V.cuda(), slots, d, block, code)
+    before = [t.clone() for t in values(cache)]
+    A.attn_cache_append(cache, K.cuda(), V.cuda(), torch.full((len(slots),), -1, device="cuda"))
+    assert all(torch.equal(a, b) for a, b in zip(before, values(cache)))
