@@ -78,9 +78,22 @@ bool usable(const attn_rows_t* t, int64_t rows) {
     return rows == 0 || t->data;
 }
 
-// An output: no two of its entries may be one.  (Rows or heads closer than d would be, wherever there are two.)
+// An output: no two of its entries may be one.  Rows or heads closer than d would be, wherever there are two ...
 bool writable(const attn_rows_t* t, int64_t rows, int32_t heads, int32_t d) {
     return usable(t, rows) && (rows <= 1 || t->ld >= d) && (heads == 1 || t->hs >= d);
+}
+
+// ... and so would row i of one head and row 0 of the h-th behind it that are closer than d: workgroups would race for them.
+bool apart(const attn_rows_t* t, int64_t rows, int32_t heads, int32_t d) {
+    if (rows <= 1 || heads <= 1) return true;
+    const __int128 ld = t->ld, hs = t->hs;
+    if (ld >= (heads - 1) * hs + d || hs >= (rows - 1) * ld + d) return true;
+    for (int32_t h = 1; h < heads; ++h)
+        for (__int128 i = h * hs / ld; i <= h * hs / ld + 1; ++i) {
+            const __int128 off = i * ld - h * hs;
+            if (i >= 1 && i < rows && off < d && off > -d) return false;
+        }
+    return true;
 }
 
 // 0 (a cap: none) or a number that 32 bits, its inverse and its quotients with another one hold with room to spare
@@ -176,6 +189,7 @@ extern "C" knn_status attn_apply(const attn_rows_t* Q, const attn_rows_t* K, con
     if (n == 0) return KNN_OK;
     st = check_workspace(plan, workspace, workspace_bytes);
     if (st != KNN_OK) return st;
+    if (!apart(O, n, hq, d)) return KNN_ERR_INVALID_ARG;
     p.q = rows_of(Q, d);
     p.k = rows_of(K, d);
     p.v = rows_of(V, d);
@@ -211,6 +225,7 @@ extern "C" knn_status attn_grad(const attn_rows_t* Q, const attn_rows_t* K, cons
     if (n == 0 && m == 0) return KNN_OK;
     st = check_workspace(plan, workspace, workspace_bytes);
     if (st != KNN_OK) return st;
+    if (!apart(dQ, n, hq, d) || !apart(dK, m, hkv, d) || !apart(dV, m, hkv, d)) return KNN_ERR_INVALID_ARG;
     p.q = rows_of(Q, d);
     p.k = rows_of(K, d);
     p.v = rows_of(V, d);
@@ -360,6 +375,7 @@ extern "C" knn_status attn_cache_apply(const attn_cache_t* cache, int32_t dtype,
         if (!workspace || reinterpret_cast<uintptr_t>(workspace) % knn::kAlign != 0) return KNN_ERR_INVALID_ARG;
         if (workspace_bytes < plan.workspace_bytes) return KNN_ERR_WORKSPACE_TOO_SMALL;
     }
+    if (!apart(O, batch * nq, hq, cache->d)) return KNN_ERR_INVALID_ARG;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     p.q = rows_of(Q, cache->d);
     p.o = rows_of(O, cache->d);

@@ -273,3 +273,15 @@ def test_rows_without_a_place_within_a_run_are_passed_over(block, code):
     before = [t.clone() for t in values(cache)]
     A.attn_cache_append(cache, K.cuda(), V.cuda(), torch.full((len(slots),), -1, device="cuda"))
     assert all(torch.equal(a, b) for a, b in zip(before, values(cache)))
+
+
+def test_outputs_whose_heads_lie_between_each_others_rows():
+    """Strides in no order that nevertheless keep every entry apart."""
+    for n, hq, ld, hs in ((2, 2, 128, 192), (3, 2, 192, 64), (2, 3, 320, 128), (40, 2, 64, 64 * 40), (5, 4, 256, 64)):
+        Q, K, V, dO = make(n, 90, hq, hq, 64, "bf16", n)
+        want = A.attn_apply(Q, K, V, GB)
+        grad = A.attn_grad(Q, K, V, *want, dO, GB)
+        views = [torch.as_strided(torch.zeros(20_000, dtype=torch.bfloat16, device="cuda"), (n, hq, 64), (ld, hs, 1)) for _ in range(2)]
+        A.attn_apply(Q, K, V, GB, out=(views[0], torch.empty_like(want[1])))
+        A.attn_grad(Q, K, V, *want, dO, GB, out=(views[1], *(torch.empty_like(t) for t in grad[1:])))
+        assert torch.equal(views[0], want[0]) and torch.equal(views[1], grad[0])
