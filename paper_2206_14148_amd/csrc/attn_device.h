@@ -432,9 +432,9 @@ __device__ __forceinline__ Joined join_ranges(const float* partial, int ranges, 
     used -= first;
     float top = -kInf, total = 0.f;
     if (lane < used) {
-        const float2 e = *reinterpret_cast<const float2*>(ends + 2 * ((first + lane) * rows + at));
-        top = e.x;
-        total = e.y;
+        const float* const e = ends + 2 * ((first + lane) * rows + at);  // (4-byte aligned: ranges, rows and d may all be odd)
+        top = e[0];
+        total = e[1];
     }
     float most = top;
 #pragma unroll

@@ -285,3 +285,20 @@ def test_outputs_whose_heads_lie_between_each_others_rows():
         A.attn_apply(Q, K, V, GB, out=(views[0], torch.empty_like(want[1])))
         A.attn_grad(Q, K, V, *want, dO, GB, out=(views[1], *(torch.empty_like(t) for t in grad[1:])))
         assert torch.equal(views[0], want[0]) and torch.equal(views[1], grad[0])
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+def test_an_odd_number_of_ranges_of_odd_rows(code):
+    """Three ranges of three heads of 37: what is kept of a range begins anywhere."""
+    d, hq, block, length = 37, 3, 16, 2090
+    plan = A.attn_cache_plan(1, 1, hq, 1, d, 2096, GB)
+    assert plan.n_ranges % 2 == 1 and plan.n_ranges > 1
+    cache = filled(131, 1, d, block, code, 6)
+    table = torch.arange(131, dtype=torch.int32, device="cuda").flip(0).contiguous()[None]
+    gen = torch.Generator().manual_seed(2)
+    for batch in (1, 3):
+        Q = torch.randn(batch, 1, hq, d, generator=gen).half().cuda()
+        lengths = [length, 700, 1][:batch]
+        got = A.attn_cache_apply(Q, cache, table.expand(batch, -1).contiguous(), words(lengths), GB).double().cpu()
+        O, most = F.cache_attention(Q, *values(cache), table.tolist() * batch, lengths, d, block)
+        assert ((got - O).abs() <= most).all()
