@@ -189,7 +189,7 @@ knn_status attn_cache_map(const int32_t *lengths, const int32_t *news, int64_t b
  * NaN becomes 0 and an infinity the largest code; neither counts for a.
  * The slots of one block must stand together in `slots`, in any order, with any that are passed over among them; of a slot given
  * twice the last counts.  Where one block's slots stand apart, with another block's between them, what becomes of that
- * block is not defined.  At most 2^27 rows times heads.
+ * block is not defined.  At most 2^27 rows times heads, and 65535 heads.
  */
 knn_status attn_cache_append(const attn_cache_t *cache, int32_t dtype, const attn_rows_t *K, const attn_rows_t *V,
                              int64_t count, const int64_t *slots, void *hip_stream);

@@ -56,7 +56,7 @@ knn_status check_shape(int64_t n, int64_t m, int32_t hq, int32_t hkv, int32_t d,
     std::memset(out, 0, sizeof(*out));
     if (n < 0 || m < 0 || hkv < 1 || hq < hkv || hq % hkv != 0 || d < 1) return KNN_ERR_INVALID_ARG;
     if (d > ATTN_MAX_D || n > kMostRows || m > kMostRows || hq > 65535) return KNN_ERR_UNSUPPORTED;
-    // rows times heads in 32 bits; one workgroup for each tile and head, at most 64 ranges each
+    // rows times heads in 32 bits, and work items of a launch: one workgroup of 256 for each tile and head (parts only where there are few)
     if ((n / attn::kTileRows + 1) * hq >= (1 << 24) || (m / attn::kTileRows + 1) * hq >= (1 << 24)) return KNN_ERR_UNSUPPORTED;
     out->n = n;
     out->m = m;
@@ -316,7 +316,7 @@ extern "C" knn_status attn_cache_append(const attn_cache_t* cache, int32_t dtype
     attn::AppendProblem p;
     if (!cache_of(cache, &p.cache) || (dtype != ATTN_BF16 && dtype != ATTN_F16) || count < 0) return KNN_ERR_INVALID_ARG;
     if (!usable(K, count) || !usable(V, count) || (count > 0 && !slots)) return KNN_ERR_INVALID_ARG;
-    if (count > kMostRows || count * cache->hkv > ((int64_t)1 << 27)) return KNN_ERR_UNSUPPORTED;
+    if (count > kMostRows || cache->hkv > 65535 || count * cache->hkv > ((int64_t)1 << 27)) return KNN_ERR_UNSUPPORTED;
     if (count == 0 || cache->blocks == 0) return KNN_OK;
     p.k = rows_of(K, cache->d);
     p.v = rows_of(V, cache->d);

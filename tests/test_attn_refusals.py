@@ -35,3 +35,10 @@ def test_outputs_whose_heads_lie_on_each_others_rows(rows, heads, ld, hs):
     if rows < 65536:
         assert lib.attn_cache_apply(cache, 0, fine, 1, rows, heads, 0x1000, 4, 0x1000, 0.1, 0.0, None, limit, *ws, out, None) == bad
     assert lib.attn_cache_apply(cache, 0, fine, rows, 1, heads, 0x1000, 4, 0x1000, 0.1, 0.0, None, limit, *ws, out, None) == bad
+
+
+def test_appends_of_more_heads_than_a_cache_can_be_read_with():
+    lib, rows = attn._load(), attn.RowsStruct(0x1000, 1 << 30, D)
+    for heads in (65536, 1 << 27):
+        cache = attn.CacheStruct(0x1000, 0x1000, 0x1000, 0x1000, 10, heads, D, 16, 0)
+        assert lib.attn_cache_append(cache, 0, rows, rows, 1, 0x1000, None) == A.KNN_ERR_UNSUPPORTED
