@@ -369,6 +369,8 @@ def attn_cache_map(lengths, news, table, free, block: int, n_slots: int, out=Non
     """
     if not lengths.is_cuda:
         _refuse("lengths must be a device tensor (no CPU path exists)")
+    if n_slots < 0:
+        _refuse("n_slots must not be negative")
     device, batch = lengths.device, lengths.numel()
     _check_table(table, batch, device)
     pointers = (_words("lengths", lengths, device, batch, torch.int32), _words("news", news, device, batch, torch.int32))

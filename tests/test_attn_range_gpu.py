@@ -7,7 +7,7 @@ import paper_2206_14148_amd as A
 torch = pytest.importorskip("torch")
 import attn_formulas as F  # noqa: E402
 from attn_bounds import STEP32, attention, compare  # noqa: E402
-from test_attn_cache_gpu import check_append, filled, values  # noqa: E402
+from test_attn_cache_gpu import check_append, check_map, filled, values  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 GB = 10 ** 9
@@ -302,3 +302,14 @@ def test_an_odd_number_of_ranges_of_odd_rows(code):
         got = A.attn_cache_apply(Q, cache, table.expand(batch, -1).contiguous(), words(lengths), GB).double().cpu()
         O, most = F.cache_attention(Q, *values(cache), table.tolist() * batch, lengths, d, block)
         assert ((got - O).abs() <= most).all()
+
+
+def test_maps_of_the_largest_batches():
+    """Their sums need more than 48 and more than 64 KiB of LDS."""
+    for batch in (6200, 16384):
+        lengths = [(37 * i) % 120 for i in range(batch)]
+        news = [(11 * i) % (n + 1) for i, n in enumerate(lengths)]
+        check_map(lengths, news, 8, 16, batch * 2, seed=batch)
+    with pytest.raises(A.KnnError) as e:
+        A.attn_cache_map(words([1]), words([1]), words([[0]]), words([0]), 16, -1)
+    assert e.value.status == A.KNN_ERR_INVALID_ARG
