@@ -53,7 +53,7 @@ struct Scores {
 
 // The power of two that ds of a lane's row (dQ) or key (dK) is taken times as an operand in f16, and that comes off the sums at the end: ds is
 // some size of <dO, V> / m, mostly below f16's normal numbers (6e-5), and with a large dO beyond its largest.  The largest
-// |<dO, V> - <dO, O>| of the first tile that has one, by which P <= 1 is multiplied yet, goes to 2^8: ds of a P of 2^-22 keeps all
+// |<dO, V> - <dO, O>| that is seen of the first tile with one, by which P <= 1 is multiplied yet, goes to 2^8: ds of a P of 2^-22 keeps all
 // its bits, and a later one has room for 2^7.  Should one be larger, the sums are not finite, and the walk that follows first looks for
 // the largest |ds|, which goes to 2^14 (scaling the sums down as it comes, as a softmax does, would not fit the registers: 550 to 700 us at
 // 4096 rows, 32 heads on 8, d = 128, f16).  bf16 has the powers of two of 32 bits.
@@ -61,7 +61,8 @@ template <typename T>
 struct Fitted {
     static constexpr bool kFits = T::kOne == F16::kOne;
     static constexpr unsigned kNone = 8u << 23;
-    unsigned inverse = kNone;  // as bits of a float
+    unsigned inverse;  // as bits of a float
+    __device__ __forceinline__ explicit Fitted(bool sees) { inverse = sees ? kNone : 127u << 23; }  // (else nothing would ever come)
     __device__ __forceinline__ bool wanted() const { return kFits && __any(inverse == kNone); }
     __device__ __forceinline__ void put(float most, int power) {
         most = max_of_halves(most);
@@ -88,10 +89,11 @@ struct Fitted {
         return __builtin_bit_cast(s16x8, r);
     }
 };
-__device__ __forceinline__ float largest(const f32x16& y) {
-    float most = fabsf(y[0]);
+template <typename Seen>
+__device__ __forceinline__ float largest(const f32x16& y, Seen seen) {
+    float most = 0.f;
 #pragma unroll
-    for (int e = 1; e < 16; ++e) most = fmaxf(most, fabsf(y[e]));
+    for (int e = 0; e < 16; ++e) most = fmaxf(most, seen(e) ? fabsf(y[e]) : 0.f);
     return most;
 }
 
@@ -150,6 +152,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     const int64_t at = (int64_t)head * p.mask.n + row;
     s16x8 q[kSteps], g[kSteps];
     float rowsum = 0.f, zero = 0.f;  // zero: NaN if an entry of Q is not finite
+    unsigned bits = 0;               // of dO: none in a row that has no part in a loss
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
         u32x4 a = {0, 0, 0, 0}, b = a, c = a;
@@ -165,6 +168,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         for (int e = 0; e < 4; ++e) {
             rowsum = __builtin_fmaf(T::low(b[e]), T::low(c[e]), rowsum);
             rowsum = __builtin_fmaf(T::high(b[e]), T::high(c[e]), rowsum);
+            bits |= b[e] & 0x7fff7fffu;
             zero = __builtin_fmaf(T::low(a[e]), 0.f, __builtin_fmaf(T::high(a[e]), 0.f, zero));
         }
     }
@@ -183,7 +187,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     if (see.inside) to.of_head(p, head);
 
     f32x16 sum[kBlocks];
-    Fitted<T> fitted;
+    Fitted<T> fitted(some && sum_of_halves(bits ? 1.f : 0.f) > 0.f);
     float most = 0.f;  // |ds|, where a walk looks for it
     Lane<DP> at_lane(lane);
     unsigned char* const keys = lds;
@@ -207,18 +211,23 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
                 x = T::mfma(at_lane.row(keys, t, k), q[k], x);
                 y = T::mfma(at_lane.row(values, t, k), g[k], y);
             }
-            if (fitted.wanted() && !look) fitted.put(largest(y), 8);
+            auto seen = [&](int from, int e) { return (unsigned)(from + 8 * (e >> 2) + (e & 3)) < (unsigned)(see.hi - see.lo); };
+            const int from_lo = j0 + 4 * half + 32 * t - see.lo;
+            if (fitted.wanted() && !look) {
+                int from = from_lo;
+                asm("" : "+v"(from));  // (or what this rarely needs is kept for the mask: registers)
+                fitted.put(largest(y, [&](int e) { return seen(from, e); }), 8);
+            }
             const float away = (float)(see.at - j0 - 4 * half - 32 * t);
             to.weights(x, y, [&](int) { return lse; }, [&](int e) { return away - (float)(8 * (e >> 2) + (e & 3)); },
                        look ? 0.f : fitted.power());
             if (edge) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if ((unsigned)(j0 + 4 * half + 32 * t + 8 * (e >> 2) + (e & 3) - see.lo) >= (unsigned)(see.hi - see.lo))
-                        y[e] = 0.f;
+                    if (!seen(from_lo, e)) y[e] = 0.f;
             }
             if (look) {
-                most = fmaxf(most, largest(y));
+                most = fmaxf(most, largest(y, [](int) { return true; }));
                 y *= 0.f;
             }
             const s16x8 w0 = rounded_operand<T>(y, 0), w1 = rounded_operand<T>(y, 1);
@@ -352,7 +361,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     }
 
     f32x16 dk[kBlocks], dv[kBlocks];
-    Fitted<T> fitted;  // of dk
+    Fitted<T> fitted(some);  // of dk
     float most = 0.f;
     Lane<DP> at_lane(lane);
     // This part's steps, of those through all rows of all heads that read K and V: from row0 of head0 to before row1 of the
@@ -398,16 +407,21 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
             y = T::mfma(at_lane.row(grads, 0, c), own_at(c), y);
             if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         }
-        if (fitted.wanted() && !look) fitted.put(largest(y), 8 - kPower);
+        auto sees = [&](int from, int e) { return (unsigned)(from + 8 * (e >> 2) + (e & 3)) < seen; };
+        if (fitted.wanted() && !look) {
+            int from = i0 + from_first;
+            asm("" : "+v"(from));
+            fitted.put(largest(y, [&](int e) { return sees(from, e); }), 8 - kPower);
+        }
         const float away = (float)(i0 + from_key);
         to.weights(x, y, [&](int e) { return -of_rows[buffer][0][8 * (e >> 2) + 4 * half + (e & 3)]; },
                    [&](int e) { return away + (float)(8 * (e >> 2) + (e & 3)); }, (float)kPower);
         if (i0 < all_low || i0 + kStepRows > all_high) {
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-                if ((unsigned)(i0 + from_first + 8 * (e >> 2) + (e & 3)) >= seen) x[e] = y[e] = 0.f;
+                if (!sees(i0 + from_first, e)) x[e] = y[e] = 0.f;
         }
-        if (look) most = fmaxf(most, largest(y));
+        if (look) most = fmaxf(most, largest(y, [](int) { return true; }));
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const s16x8 weights = rounded_operand<T>(x, c), slopes = fitted.operand(y, c, look);

@@ -6,8 +6,8 @@ Bounds, u = eps / 2 of the type:
               score itself (the kernels have two forms of tanh); slopes and the exponential a few steps of what they act on
   a weight    rounded once to the type, f16 with its powers of two moved up: by 2^7 and more above the largest one,
               so that half of the smallest step, 2^-25, is 2^-32 of it; in dV by 2^14: 2^-39
-  ds          rounded once to the type, f16 times a power of two that puts the largest |<dO, V> - <dO, O>| of some rows and keys at
-              2^8 or more, or the largest |ds| at 2^14: half of the smallest step is 2^-33 of the largest of all
+  ds          rounded once to the type, f16 times a power of two that puts the largest |<dO, V> - <dO, O>| of some of what is seen at 2^8 or
+              more, or the largest |ds| at 2^14: half of the smallest step is 2^-33 of the largest that is seen
 """
 import math
 
@@ -56,13 +56,9 @@ def attention(Q, K, V, dO=None, scale=None, causal=False, cap=0.0, slopes=None, 
         for f in range(hkv):
             k, v = K[k0:k1, f], V[k0:k1, f]
             all_ds, all_off, all_q, all_seen = [], [], [], []
-            if dO is not None:  # |<dO, V> - <dO, O>| at most, by rows and heads, and by keys (O is a mean of V)
-                met = torch.nan_to_num(dO[:, f * group:(f + 1) * group].flatten(0, 1) @ V[:, f].T, 0, 0, 0).abs()
-                by_row = met.amax(1, keepdim=True) if m else torch.zeros(n * group, 1).double()
-                by_key = (met + by_row).amax(0)[k0:k1, None] if n else None
-                by_row = 2 * by_row.view(n, group)
             for name in ("dK", "dV"):
                 r[name][k0:k1, f] = 0.0
+            by_key = torch.zeros(nk, 1, dtype=torch.float64)  # |<dO, V> - <dO, O>| of who sees a key, at most
             for h in range(f * group, (f + 1) * group):
                 q = Q[q0:q1, h]
                 finite_k, finite_q = torch.nan_to_num(k, 0, 0, 0).abs(), torch.nan_to_num(q, 0, 0, 0).abs()
@@ -119,7 +115,10 @@ def attention(Q, K, V, dO=None, scale=None, causal=False, cap=0.0, slopes=None, 
                     off_ds = off_ds + torch.nan_to_num(P * raw.abs(), 0, 0, 0) * (2 * off / cap + 16 * STEP32)
                 off_ds = torch.where(seen, off_ds, torch.zeros_like(off_ds))
                 all_ds.append(ds), all_off.append(off_ds), all_q.append(q), all_seen.append(seen)
-                most = by_row[q0:q1, h - f * group, None]
+                met = torch.where(seen, torch.nan_to_num(g0 @ v.T, 0, 0, 0).abs(), torch.zeros_like(P))
+                most = 2 * met.amax(1, keepdim=True) if nk else torch.zeros(nq, 1).double()  # (O is a mean of V)
+                if nq and nk:
+                    by_key = torch.maximum(by_key, torch.where(seen, met + most / 2, torch.zeros_like(met)).amax(0)[:, None])
                 dQ = scale * _masked(ds, seen, k)
                 # one of K that is not finite: NaN in dQ of the rows that see it
                 meets = (seen & ~torch.isfinite(k).all(1)[None]).any(1)
