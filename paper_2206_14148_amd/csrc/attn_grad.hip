@@ -291,14 +291,13 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         done = entries == kFinite || all_finite();
     }
     if (!see.inside) return;
-    const float times = none ? 0.f : lost ? __builtin_nanf("") : p.scale * fitted.back();
-    if (none) begin();
+    const float times = lost ? __builtin_nanf("") : p.scale * fitted.back();
     if (p.row_splits > 1) {
         float* const parts = p.row_partial + (split * (int64_t)p.hq * p.mask.n + at) * p.d;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int a = 0; a < 4; ++a) put4(parts, 32 * b + 8 * a + 4 * half, p.d, sum[b] * times, 4 * a);
+            for (int a = 0; a < 4; ++a) put4(parts, 32 * b + 8 * a + 4 * half, p.d, none ? f32x16{} : sum[b] * times, 4 * a);
         return;
     }
     unsigned short* const o = p.dq.data + row * p.dq.ld + head * p.dq.hs;
@@ -308,7 +307,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         for (int a = 0; a < 4; ++a) {
             float x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = sum[b][4 * a + e] * times;
+            for (int e = 0; e < 4; ++e) x[e] = none ? 0.f : sum[b][4 * a + e] * times;
             put4<T>(o, 32 * b + 8 * a + 4 * half, p.d, p.dq.wide, x);
         }
 }
@@ -391,16 +390,19 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
         const unsigned own = at_lane.rows ^ (buffer ? L::kBytes : 0);
         auto own_at = [&](int c) { return *reinterpret_cast<const s16x8*>(own_values + (own ^ (32 * c))); };
         f32x16 x, y;
+        auto of_all = [&](f32x16& to_x, int which) {
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const f32x4 lse = to.capped ? f32x4{} : *reinterpret_cast<const f32x4*>(&of_rows[buffer][0][8 * a + 4 * half]);
-            const f32x4 rowsum = *reinterpret_cast<const f32x4*>(&of_rows[buffer][1][8 * a + 4 * half]);
+            for (int a = 0; a < 4; ++a) {
+                const f32x4 four = *reinterpret_cast<const f32x4*>(&of_rows[buffer][which][8 * a + 4 * half]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[4 * a + e] = lse[e];
-                y[4 * a + e] = rowsum[e];
+                for (int e = 0; e < 4; ++e) to_x[4 * a + e] = four[e];
             }
-        }
+        };
+        if (to.capped)
+            x = f32x16{};
+        else
+            of_all(x, 0);
+        of_all(y, 1);
 #pragma unroll
         for (int c = 0; c < kSteps; ++c) {
             x = T::mfma(at_lane.row(queries, 0, c), k[c], x);
