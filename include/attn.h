@@ -137,8 +137,9 @@ knn_status attn_grad(const attn_rows_t *Q, const attn_rows_t *K, const attn_rows
  *
  * What answers one row at a time keeps the K and V of the rows before it.  Here they lie as 8-bit codes
  * in blocks of `block` rows ("tokens"), in any order; a table gives each request its blocks, and every
- * block has a scale for each head: a value is code * scale.  Half the bytes of 16-bit rows, and less
- * than a hundredth on top for the scales: with a limit on device memory, twice the history.
+ * block has a scale for each head: a value is code * scale.  With rows of 64 or 128 entries half the bytes of 16-bit rows, and
+ * less than a hundredth on top for the scales: with a limit on device memory, twice the history.  (Rows are kept
+ * 64 or 128 wide, so others gain less: one of 96 takes two thirds of its 16-bit bytes, one below 32 more than those.)
  *
  *   k  [blocks][hkv][block][row]   codes, a token's entries together
  *   v  [blocks][hkv][row][block]   codes, an entry's tokens together: the product with V sums over tokens

@@ -230,8 +230,8 @@ def attn_apply(Q, K, V, mem_limit_bytes: int, scale=None, causal: bool = False, 
     become cap * tanh(score / cap); slopes fp32 [hq]: minus slope * distance; starts, k_starts int32
     [docs + 1] (k_starts = starts unless given): rows see keys of their own document; prefix int32
     [docs]: keys at a document's start that all its rows see although causal.  Rows outside the
-    documents keep what `out` (O, lse) holds there.  The workspace (uint8, attn_plan's bytes) is
-    allocated here unless given.  Work is enqueued on torch's current stream; no synchronisation is done.
+    documents keep what `out` (O, lse) holds there.  d is 128 at most.  The call is not recorded for autograd, whatever
+    its inputs ask for: attn_grad gives the gradients.  The workspace (uint8, attn_plan's bytes) is allocated here unless given.  Work is enqueued on torch's current stream; no synchronisation is done.
     """
     n, m, hq, hkv, d = _shape(Q, K, V)
     plan = _planned(_load().attn_plan, AttnPlanStruct(), n, m, hq, hkv, d, mem_limit_bytes)
@@ -265,7 +265,8 @@ def attn_grad(Q, K, V, O, lse, dO, mem_limit_bytes: int, scale=None, causal: boo
 
     The gradients of sum(dO * O) by Q, K and V; O and lse as attn_apply gave them for the same Q, K, V and
     options.  Heads that share a K and V add up.  The workspace (uint8, attn_grad_plan's bytes) is allocated here
-    unless given; `out` takes the three gradients.  The same inputs give the same bits.
+    unless given; `out` takes the three gradients.  The same inputs give the same bits.  In float16 P and the scores'
+    gradients are scaled by powers of two, so dO may be of any magnitude that its gradients have in float16.
     """
     n, m, hq, hkv, d = _shape(Q, K, V)
     _check_rows("O", O, Q, (n, hq, d))

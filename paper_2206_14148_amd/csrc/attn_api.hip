@@ -23,7 +23,7 @@ constexpr int64_t kMostRows = (int64_t)1 << 30;
 // to be written and read at 4 TB/s, and their join is a launch of 5 us.  A workgroup's walk ends no earlier than its
 // own steps, all workgroups' no earlier than 2 to a compute unit allow; `share` is the part of the steps that the mean
 // workgroup has (by keys half, as with a causal mask, where the first keys' workgroups have all).
-// 3 rows of 16 heads against 50021 keys: 854 us in one part, 25 in 256; 1201 rows of 8 heads: 27 in one, 22 in 4, 27 in 8;
+// 3 rows of 16 heads against 50021 keys: 854 us in one part, 25 in 128; 1201 rows of 8 heads: 27 in one, 22 in 4, 27 in 8;
 // the gradient of 4096 rows of 32 heads: 1000 in one, 575 in 4.
 int best_parts(int64_t workgroups, int64_t steps, double share, double bytes_a_part, uint64_t room, uint64_t (*bytes)(const int64_t*, int64_t),
                const int64_t* shape) {

@@ -155,8 +155,8 @@ __device__ __forceinline__ float quotient_of(float code, float from, float to) {
 // A workgroup looks at `tokens` new rows for one head; where the first row of a run of rows that go to one block is among
 // them it does the run.  What bounds it for a step's few rows is one memory access waiting for another: slots, then rows and
 // scales, then the codes go out (8 us for one row, 12 for 64 rows and 8 heads, of which a launch is 3).  Blocks of up to 32
-// tokens take a wave, whose lanes need not wait for each other (9216 rows of 128, 8 heads, blocks of 16: 31 us, with four
-// waves 69), larger ones four (64 rows, blocks of 64: 15 us, with one wave 40; 9216 rows 92).  Rows are kept in registers from the
+// tokens take a wave, whose lanes need not wait for each other (9216 rows of 128, 8 heads, blocks of 16: 34 us, with four
+// waves 69), larger ones four (64 rows, blocks of 64: 13 us, with one wave 40; 9216 rows 92).  Rows are kept in registers from the
 // search of the largest magnitude to the codes where they fit, else read again.  A block's codes of V lie across its rows, so
 // they are put together in LDS and written a word of four tokens at a time; a word that the run fills in part, and that is not
 // begun anew, is written byte by byte.
@@ -455,8 +455,8 @@ __device__ __forceinline__ f32x4 codes_mfma(u32x2 w, s16x8 q, f32x4 c) {
 // that the lanes of group g = l / 16 get the scores of tokens 16 g .. 16 g + 15, which lie in one block; a lane reads
 // its quarter of a token's row.  V: a lane reads one entry's tokens 16 g .. 16 g + 15, 16 bytes, and its scores,
 // rounded, are the other operand as they are.  Nothing goes through LDS until the four waves' sums meet.  Bound by reading the
-// codes: 200003 tokens of 8 heads of 128 in 86 us, 4.8 TB/s with the join, as fast as a large copy here; 64 requests of 512 to
-// 8192 tokens in 136 us, 4.2 TB/s: the last workgroups end one after the other.
+// codes: 200003 tokens of 8 heads of 128 in 87 us, 4.7 TB/s with the join, as fast as a large copy here; 64 requests of 512 to
+// 8192 tokens in 134 us, 4.2 TB/s: the last workgroups end one after the other.
 template <typename T, bool E4M3, int ROW, int SETS>
 __global__ __launch_bounds__(256) void attn_cache_kernel(CacheProblem p) {
     constexpr int kSteps = ROW / 32, kTiles = ROW / 16;

@@ -64,9 +64,11 @@ __device__ __forceinline__ void write_rows(const Problem& p, const Span& see, in
 
 // Four waves of 32 rows; a step takes 64 keys, whose K and V go straight to LDS while the last step's are worked on (64 KiB, two
 // workgroups on a compute unit, one's exponentials beside the other's products).  8192 rows, causal, 32 heads on 8, d = 128,
-// bf16: 540 us, 1020 TFLOP/s (a large matrix product reaches 1390 here).  Matrix cores are busy for half of the time, the vector
-// unit (a maximum, a product, an exponential, a sum and half a conversion for each score) for about as much, and
-// the clock falls to 1.8 GHz: an order of instructions that kept the matrix cores 14 % busier took the same time.
+// bf16: 541 us, 1020 TFLOP/s (a large matrix product reaches 1390 here).  Matrix cores are busy for 53 % of the cycles.  A wave has one
+// set of rows, so every MFMA reads 1 KB of its own from LDS: at 128 bytes a cycle another 53 %, with the tiles' writes and
+// conflicts four fifths.  The vector unit (a maximum, a product, an exponential, a sum and half a conversion for each score)
+// is busy for about half as well, and the clock falls to 1.8 GHz: an order of instructions that kept the matrix cores
+// 14 % busier took the same time.  Which of them binds was not separated.
 // With a cap another exponential and a reciprocal come to each score, and the vector unit alone bounds it.
 template <typename T, int DP, bool LARGE_CAP>  // cap > kLargeCap
 __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {

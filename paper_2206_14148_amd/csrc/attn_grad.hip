@@ -315,8 +315,9 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
 // By keys a step takes 32 rows, and V, the second operand of only one product, stays in LDS: so two workgroups share a
 // compute unit, one's exponentials beside the other's products.  4096 rows and keys, causal, 32 heads on 8, d = 128, bf16: 345 us
 // or 800 TFLOP/s of its four products (with V in registers and 64 rows a step one workgroup, and 444 us); the walk by rows
-// takes 245 us for its three, 840 TFLOP/s.  What bounds both is the matrix cores' share: the vector instructions of the
-// exponentials (some 10 for a score) take nearly as long as the products, and hide behind the other workgroup's only in part.
+// takes 247 us for its three, 830 TFLOP/s.  Matrix cores are busy for 44 and 48 % of the cycles; their operands from LDS, 1 KB for
+// an MFMA (by keys a quarter more, V's), take 55 and 48 % of them at 128 bytes a cycle, the tiles' writes and conflicts 17 and 16 %;
+// the vector instructions of the exponentials (some 10 for a score) hide behind the other workgroup's products only in part.
 template <typename T, int DP, bool LARGE_CAP>
 __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     typedef Tile<DP, kStepRows> L;
