@@ -160,7 +160,7 @@ __device__ __forceinline__ float quotient_of(float code, float from, float to) {
 // search of the largest magnitude to the codes where they fit, else read again.  A block's codes of V lie across its rows, so
 // they are put together in LDS and written a word of four tokens at a time; a word that the run fills in part, and that is not
 // begun anew, is written byte by byte.
-// e4m3 needs few enough registers for a fifth wave on a SIMD (append of 8 prompts of up to 2048 rows, blocks of 64: 136 us with the
+// e4m3 needs few enough registers for a fifth wave on a SIMD (append of 8 prompts of up to 2048 rows, blocks of 64: 135 us with the
 // values that are looked at, 144 with four).
 constexpr int kAppendPasses = 4;
 constexpr int kAhead = 8;  // loads of slots under way together where rows without a place are passed over
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(THREADS, E4M3 ? 5 : 4) void attn_append_kernel(Appe
     __shared__ unsigned char moved_to[2][256];  // what becomes of each code that the block holds
     __shared__ float of_wave[2][THREADS / 64];
     __shared__ int run_end, run_last, run_hole;
-    const int tid = threadIdx.x;
+    const int thread = threadIdx.x;
     const int head = blockIdx.x % c.hkv, shift = __builtin_ctz(c.block), pitch = c.block + 4;
     const int64_t group = (int64_t)(blockIdx.x / c.hkv) * tokens, slots = c.blocks << shift;
     auto block_of = [&](int64_t t) {  // -1: none
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(THREADS, E4M3 ? 5 : 4) void attn_append_kernel(Appe
         return s >= 0 && s < slots ? (int)(s >> shift) : -1;
     };
     // lane l of each wave: whether a run begins at row group + l
-    const int lane = tid & 63;
+    const int lane = thread & 63;
     const int mine = lane < tokens ? block_of(group + lane) : -1;
     int before_mine = lane < tokens ? block_of(group + lane - 1) : -1;
     if (__any(mine >= 0 && before_mine < 0 && group + lane > 0)) {
@@ -207,8 +207,10 @@ __global__ __launch_bounds__(THREADS, E4M3 ? 5 : 4) void attn_append_kernel(Appe
         if (!below) before_mine = before;
     }
     unsigned long long firsts = __ballot(mine >= 0 && mine != before_mine);
-    const int pieces = c.row / 8, per_pass = THREADS / pieces, piece = tid % pieces, line = tid / pieces;
+    const int pieces = c.row / 8, per_pass = THREADS / pieces, piece = thread % pieces, line = thread / pieces;
     while (firsts) {
+        int tid = thread;
+        asm volatile("" : "+v"(tid));  // (or addresses made of it are kept from run to run: registers)
         const int64_t first = group + __builtin_ctzll(firsts);
         const int block = block_of(first);
         const int64_t at = (int64_t)block * c.hkv + head;

@@ -109,6 +109,13 @@ __device__ __forceinline__ int wave_most(int v) {
     return __builtin_amdgcn_readfirstlane(v);
 }
 
+// The lane's number made anew, for what comes behind a walk: no register keeps it, or threadIdx, meanwhile.
+__device__ __forceinline__ int lane_again() {
+    int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // ---- documents --------------------------------------------------------------------------------
 
 // The document that holds x, by its starts: the last one that begins at or before x; -1 if x lies outside all.

@@ -264,7 +264,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
             tile_of(j0, keys, false);
         }
         done = all_finite();
-        at_lane = Lane<DP>(lane);
+        at_lane = Lane<DP>(lane_again());
         entries = kFinite;
     }
     // Without 16-byte reads; and where a sum came out not finite.  An entry of K that is not finite meets the zero weights
@@ -275,13 +275,14 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
         for (int look = Fitted<T>::kFits && entries == kFinite; look >= 0; --look) {
             begin();
             for (int j0 = first; j0 < last; j0 += kTileKeys) {
+                const int own_tid = 64 * wave + lane_again();
                 arrive_and_wait();
-                stage<T, DP, 256>(keys, p.k, kv, j0, first, last, p.d, tid, kAsTheyAre);
-                stage<T, DP, 256>(values, p.v, kv, j0, first, last, p.d, tid, kAsTheyAre);
-                if (entries == kFinite) stage<T, DP, 256>(keys + L::kBytes, p.k, kv, j0, first, last, p.d, tid, kFinite);
+                stage<T, DP, 256>(keys, p.k, kv, j0, first, last, p.d, own_tid, kAsTheyAre);
+                stage<T, DP, 256>(values, p.v, kv, j0, first, last, p.d, own_tid, kAsTheyAre);
+                if (entries == kFinite) stage<T, DP, 256>(keys + L::kBytes, p.k, kv, j0, first, last, p.d, own_tid, kFinite);
                 arrive_and_wait();
                 if (entries == kFinite) {
-                    const uint64_t bad = not_finite<T, L>(keys, lane);
+                    const uint64_t bad = not_finite<T, L>(keys, own_tid & 63);
                     lost = lost || (bad & bits_between(see.lo - j0, see.hi - j0));
                 }
                 tile_of(j0, entries == kFinite ? keys + L::kBytes : keys, look);
@@ -292,15 +293,18 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
     }
     if (!see.inside) return;
     const float times = lost ? __builtin_nanf("") : p.scale * fitted.back();
+    // (made again here rather than kept from where it was first needed)
+    const int own_lane = lane_again(), own_half = own_lane >> 5, own_line = tile * kTileRows + wave * 32 + (own_lane & 31);
+    const int own_row = own_line / group, own_head = kv * group + own_line % group;
     if (p.row_splits > 1) {
-        float* const parts = p.row_partial + (split * (int64_t)p.hq * p.mask.n + at) * p.d;
+        float* const parts = p.row_partial + ((split * (int64_t)p.hq + own_head) * p.mask.n + own_row) * p.d;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int a = 0; a < 4; ++a) put4(parts, 32 * b + 8 * a + 4 * half, p.d, none ? f32x16{} : sum[b] * times, 4 * a);
+            for (int a = 0; a < 4; ++a) put4(parts, 32 * b + 8 * a + 4 * own_half, p.d, none ? f32x16{} : sum[b] * times, 4 * a);
         return;
     }
-    unsigned short* const o = p.dq.data + row * p.dq.ld + head * p.dq.hs;
+    unsigned short* const o = p.dq.data + own_row * p.dq.ld + own_head * p.dq.hs;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -308,7 +312,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
             float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = none ? 0.f : sum[b][4 * a + e] * times;
-            put4<T>(o, 32 * b + 8 * a + 4 * half, p.d, p.dq.wide, x);
+            put4<T>(o, 32 * b + 8 * a + 4 * own_half, p.d, p.dq.wide, x);
         }
 }
 
@@ -379,7 +383,9 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
         for (int b = 0; b < kBlocks; ++b) dk[b] = dv[b] = f32x16{};
     };
     // of a lane's first row of a tile: how far past the key it stands, and past the first row that sees the key
-    const int from_key = see.at - key + 4 * half, from_first = 4 * half - see.lo;
+    int from_key = see.at - key + 4 * half;
+    asm("" : "+v"(from_key));  // (or what it is made of is kept as well)
+    const int from_first = 4 * half - see.lo;
     const unsigned seen = see.hi - see.lo;
     // 32 rows that lie in LDS.
     Scores<LARGE_CAP, Fitted<T>::kFits> to(p);
@@ -472,7 +478,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
             }
         }
         done = all_finite();
-        at_lane = Lane<DP>(lane);
+        at_lane = Lane<DP>(lane_again());
         entries = kFinite;
     }
     // Entries of Q and dO that are not finite as zeros in a second walk.  Their rows have a log-sum that the walk by rows
@@ -484,10 +490,11 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
                 to.of_head(p, head);
                 const int end = head + 1 < head1 ? last : row1;
                 for (int i0 = head == head0 ? row0 : first; i0 < end; i0 += kStepRows) {
+                    const int own_lane = lane_again(), own_tid = 64 * wave + own_lane;
                     arrive_and_wait();
-                    stage<T, DP, 256, kStepRows>(queries, p.q, head, i0, first, last, p.d, tid, entries);
-                    stage<T, DP, 256, kStepRows>(grads, p.dO, head, i0, first, last, p.d, tid, entries);
-                    if (wave < 2 && lane < kStepRows) of_rows[0][wave][lane] = i0 + lane < last ? sums_of(wave, head, i0)[lane] : 0.f;
+                    stage<T, DP, 256, kStepRows>(queries, p.q, head, i0, first, last, p.d, own_tid, entries);
+                    stage<T, DP, 256, kStepRows>(grads, p.dO, head, i0, first, last, p.d, own_tid, entries);
+                    if (wave < 2 && own_lane < kStepRows) of_rows[0][wave][own_lane] = i0 + own_lane < last ? sums_of(wave, head, i0)[own_lane] : 0.f;
                     arrive_and_wait();
                     tile_of(i0, 0, look);
                 }
@@ -498,10 +505,8 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
     }
     if (!see.inside) return;
     // (made again here rather than kept, in registers or beside them, from where it was first needed)
-    int tid_again = threadIdx.x;
-    asm("" : "+v"(tid_again));
-    const int half_again = (tid_again >> 5) & 1;
-    const int64_t row = tile * kTileRows + (tid_again >> 6) * 32 + (tid_again & 31);
+    const int lane_here = lane_again(), half_again = lane_here >> 5;
+    const int64_t row = tile * kTileRows + wave * 32 + (lane_here & 31);
     const float times = p.scale * kBack * fitted.back();
     if (p.splits > 1) {
         const int64_t keys = (int64_t)p.mask.m * p.hkv;
