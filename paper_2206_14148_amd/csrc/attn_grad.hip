@@ -53,8 +53,8 @@ struct Scores {
 
 // The power of two that ds of a lane's row (dQ) or key (dK) is taken times as an operand in f16, and that comes off the sums at the end: ds is
 // some size of <dO, V> / m, mostly below f16's normal numbers (6e-5), and with a large dO beyond its largest.  The largest
-// |<dO, V> - <dO, O>| that is seen of the first tile with one, by which P <= 1 is multiplied yet, goes to 2^8: ds of a P of 2^-22 keeps all
-// its bits, and a later one has room for 2^7.  Should one be larger, the sums are not finite, and the walk that follows first looks for
+// |<dO, V> - <dO, O>| that is seen of the first tile with one, by which P <= 1 is multiplied yet, goes to 2^8 (or <dO, O>: of a row that sees
+// one key the difference is nothing but rounding): ds of a P of 2^-22 keeps all its bits, and a later one has room for 2^7.  Should one be larger, the sums are not finite, and the walk that follows first looks for
 // the largest |ds|, which goes to 2^14 (scaling the sums down as it comes, as a softmax does, would not fit the registers: 550 to 700 us at
 // 4096 rows, 32 heads on 8, d = 128, f16).  bf16 has the powers of two of 32 bits.
 template <typename T>
@@ -63,7 +63,11 @@ struct Fitted {
     static constexpr unsigned kNone = 8u << 23;
     unsigned inverse;  // as bits of a float
     __device__ __forceinline__ explicit Fitted(bool sees) { inverse = sees ? kNone : 127u << 23; }  // (else nothing would ever come)
-    __device__ __forceinline__ bool wanted() const { return kFits && __any(inverse == kNone); }
+    // Whether a lane has none yet of those that see something of 32 keys (rows) of a tile; `from`: how far the lane's first of them, which is the
+    // tile's first or fourth, is behind the first that it sees of `seen`.
+    __device__ __forceinline__ bool wanted(int from, unsigned seen) const {
+        return kFits && __any(inverse == kNone && (unsigned)(from + 31) < seen + 35u);
+    }
     __device__ __forceinline__ void put(float most, int power) {
         most = max_of_halves(most);
         if (inverse == kNone && most > 0.f && most < kInf) inverse = min(max((int)(__float_as_uint(most) >> 23) - power, 9), 246) << 23;
@@ -89,11 +93,11 @@ struct Fitted {
         return __builtin_bit_cast(s16x8, r);
     }
 };
-template <typename Seen>
-__device__ __forceinline__ float largest(const f32x16& y, Seen seen) {
+template <typename Size>
+__device__ __forceinline__ float largest(Size size) {  // of 16
     float most = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) most = fmaxf(most, seen(e) ? fabsf(y[e]) : 0.f);
+    for (int e = 0; e < 16; ++e) most = fmaxf(most, size(e));
     return most;
 }
 
@@ -213,10 +217,10 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
             }
             auto seen = [&](int from, int e) { return (unsigned)(from + 8 * (e >> 2) + (e & 3)) < (unsigned)(see.hi - see.lo); };
             const int from_lo = j0 + 4 * half + 32 * t - see.lo;
-            if (fitted.wanted() && !look) {
+            if (!look && fitted.wanted(from_lo, see.hi - see.lo)) {
                 int from = from_lo;
                 asm("" : "+v"(from));  // (or what this rarely needs is kept for the mask: registers)
-                fitted.put(largest(y, [&](int e) { return seen(from, e); }), 8);
+                fitted.put(largest([&](int e) { return seen(from, e) ? fmaxf(fabsf(y[e]), fabsf(rowsum)) : 0.f; }), 8);
             }
             const float away = (float)(see.at - j0 - 4 * half - 32 * t);
             to.weights(x, y, [&](int) { return lse; }, [&](int e) { return away - (float)(8 * (e >> 2) + (e & 3)); },
@@ -227,7 +231,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_rows_kernel(Problem p) {
                     if (!seen(from_lo, e)) y[e] = 0.f;
             }
             if (look) {
-                most = fmaxf(most, largest(y, [](int) { return true; }));
+                most = fmaxf(most, largest([&](int e) { return fabsf(y[e]); }));
                 y *= 0.f;
             }
             const s16x8 w0 = rounded_operand<T>(y, 0), w1 = rounded_operand<T>(y, 1);
@@ -417,10 +421,17 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
             if (c % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         }
         auto sees = [&](int from, int e) { return (unsigned)(from + 8 * (e >> 2) + (e & 3)) < seen; };
-        if (fitted.wanted() && !look) {
+        if (!look && fitted.wanted(i0 + from_first, seen)) {
             int from = i0 + from_first;
             asm("" : "+v"(from));
-            fitted.put(largest(y, [&](int e) { return sees(from, e); }), 8 - kPower);
+            float most = 0.f;
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                const f32x4 rowsum = *reinterpret_cast<const f32x4*>(&of_rows[buffer][1][8 * a + 4 * half]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = fmaxf(most, sees(from, 4 * a + e) ? fmaxf(fabsf(y[4 * a + e]), fabsf(rowsum[e])) : 0.f);
+            }
+            fitted.put(most, 8 - kPower);
         }
         const float away = (float)(i0 + from_key);
         to.weights(x, y, [&](int e) { return -of_rows[buffer][0][8 * (e >> 2) + 4 * half + (e & 3)]; },
@@ -430,7 +441,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
             for (int e = 0; e < 16; ++e)
                 if (!sees(i0 + from_first, e)) x[e] = y[e] = 0.f;
         }
-        if (look) most = fmaxf(most, largest(y, [](int) { return true; }));
+        if (look) most = fmaxf(most, largest([&](int e) { return fabsf(y[e]); }));
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const s16x8 weights = rounded_operand<T>(x, c), slopes = fitted.operand(y, c, look);
