@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
         }
     };
     // A tile's products x to what the weights are the exponentials of.
-    auto scores = [&](f32x16* x, int j0) {
+    auto scores = [&](f32x16* x, int j0, bool marks) {
         if (LARGE_CAP) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
         if (__any(most > most_over)) {
             const bool none = most_over != slack;
             const float up = none ? (most == -kInf ? 0.f : most - lift) : fmaxf(most - lift, 0.f);
-            const float shrink = none ? 1.f : __builtin_amdgcn_exp2f(-up * factor);
+            const float shrink = none || marks ? 1.f : __builtin_amdgcn_exp2f(-up * factor);
             if (most > -kInf) most_over = slack;
             top += up;
             total *= shrink;
@@ -186,12 +186,13 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(Problem p) {
             for (int t = 0; t < 2; ++t) x[t] -= up;
         }
     };
-    // One tile that lies in LDS.  marks: with a weight of one for every key that is seen (and has a score above -infinity).
+    // One tile that lies in LDS.  marks: with a weight of one for every key that is seen (and has a score
+    // above -infinity), whatever comes behind it.
     auto tile_of = [&](int j0, bool marks) {
         if (j0 >= high || j0 + kTileKeys <= low) return;
         f32x16 x[2];
         products(x);
-        scores(x, j0);
+        scores(x, j0, marks);
         if (marks) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)

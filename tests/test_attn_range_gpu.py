@@ -109,10 +109,12 @@ def test_infinities_of_v_behind_small_weights(dtype, reading):
             Q[:, :, 0] = 8.0
             K[:, :, 0] = -away
             K[7, :, 0] = 0.0
+            K2 = K.roll(m - 10, 0)  # what outweighs them before them, and far behind them
             for value in (INF, -INF, float("nan")):
                 W = V.clone()
                 W[m - 30, 0, 5] = value
                 W[11, 0, 9] = value
+                check(Q, K2, W, None, names=NAMES[:2])
                 if reading == "entries":
                     check(odd(Q), odd(K), odd(W), None, names=NAMES[:2])
                 else:
