@@ -187,7 +187,7 @@ knn_status attn_cache_map(const int32_t *lengths, const int32_t *news, int64_t b
  * codes zero and its scale 0.  scale' = max(scale, fl(a / most)), a the largest magnitude of the new rows,
  * most = 127 or 448, fl to fp32.  If scale' > scale the codes there become the nearest to code * scale / scale'.
  * A new code is the nearest to x / scale' (of two as near the even one; quotients of real numbers).
- * NaN becomes 0 and an infinity the largest code; neither counts for a.
+ * NaN becomes 0 and an infinity the largest code; neither counts for a.  (Of a scale of 0 every code is 0.)
  * The slots of one block must stand together in `slots`, in any order, with any that are passed over among them; of a slot given
  * twice the last counts.  Where one block's slots stand apart, with another block's between them, what becomes of that
  * block is not defined.  At most 2^27 rows times heads, and 65535 heads.
