@@ -53,8 +53,9 @@ struct Scores {
 
 // The power of two that ds of a lane's row (dQ) or key (dK) is taken times as an operand in f16, and that comes off the sums at the end: ds is
 // some size of <dO, V> / m, mostly below f16's normal numbers (6e-5), and with a large dO beyond its largest.  The largest
-// |<dO, V> - <dO, O>| that is seen of the first tile with one, by which P <= 1 is multiplied yet, goes to 2^8 (or <dO, O>: of a row that sees
-// one key the difference is nothing but rounding): ds of a P of 2^-22 keeps all its bits, and a later one has room for 2^7.  Should one be larger, the sums are not finite, and the walk that follows first looks for
+// |<dO, V> - <dO, O>| that is seen of the first tile with one, by which P <= 1 is multiplied yet, goes to 2^8 for a row, to 2^4 for a key
+// (or <dO, O>: of a row that sees one key the difference is nothing but rounding): ds of a P of 2^-22 and 2^-18 keeps all its bits, and a later
+// one has room for 2^7, and 2^11 by keys, whose rows' dO may be of many magnitudes.  Should one be larger, the sums are not finite, and the walk that follows first looks for
 // the largest |ds|, which goes to 2^14 (scaling the sums down as it comes, as a softmax does, would not fit the registers: 550 to 700 us at
 // 4096 rows, 32 heads on 8, d = 128, f16).  bf16 has the powers of two of 32 bits.
 template <typename T>
@@ -431,7 +432,7 @@ __global__ __launch_bounds__(256, 2) void attn_grad_keys_kernel(Problem p) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) most = fmaxf(most, sees(from, 4 * a + e) ? fmaxf(fabsf(y[4 * a + e]), fabsf(rowsum[e])) : 0.f);
             }
-            fitted.put(most, 8 - kPower);
+            fitted.put(most, 4 - kPower);
         }
         const float away = (float)(i0 + from_key);
         to.weights(x, y, [&](int e) { return -of_rows[buffer][0][8 * (e >> 2) + 4 * half + (e & 3)]; },

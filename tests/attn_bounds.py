@@ -6,8 +6,8 @@ Bounds, u = eps / 2 of the type:
               score itself (the kernels have two forms of tanh); slopes and the exponential a few steps of what they act on
   a weight    rounded once to the type, f16 with its powers of two moved up: by 2^7 and more above the largest one,
               so that half of the smallest step, 2^-25, is 2^-32 of it; in dV by 2^14: 2^-39
-  ds          rounded once to the type, f16 times a power of two that puts the largest |<dO, V> - <dO, O>| of some of what is seen at 2^8 or
-              more, or the largest |ds| at 2^14: half of the smallest step is 2^-33 of the largest that is seen
+  ds          rounded once to the type, f16 times a power of two that puts the largest |<dO, V> - <dO, O>| of some of what is seen at 2^8
+              (dK: 2^4) or more, or the largest |ds| at 2^14: half of the smallest step is 2^-33 (2^-29) of the largest that is seen
 """
 import math
 
@@ -135,7 +135,7 @@ def attention(Q, K, V, dO=None, scale=None, causal=False, cap=0.0, slopes=None, 
                 size_q = torch.nan_to_num(q, 0, 0, 0).abs()
                 r["dK"][k0:k1, f] += scale * _masked(ds.T, seen.T, q)
                 r["dK+"][k0:k1, f] += 1.01 * scale * ((off_ds + (nq * hq + 4) * STEP32 * torch.nan_to_num(ds, 0, 0, 0).abs()).T @ size_q +
-                                                      small_ds * by_key * (seen.double().T @ size_q))
+                                                      16 * small_ds * by_key * (seen.double().T @ size_q))
     for c in range(len(starts) - 1):  # a gradient that is not finite: whichever way
         for name, at in (("dQ", slice(starts[c], starts[c + 1])), ("dK", slice(k_starts[c], k_starts[c + 1])),
                          ("dV", slice(k_starts[c], k_starts[c + 1]))):
